@@ -56,7 +56,8 @@ extern "C" {
 typedef enum mdss_status {
   MDSS_OK = 0,
   MDSS_EINVAL = 1,       /* null pointer or invalid argument value */
-  MDSS_ESHAPE = 2,       /* B outside [0, MDSS_MAX_B] or V outside [2, MDSS_MAX_V] */
+  MDSS_ESHAPE = 2,       /* B outside [0, MDSS_MAX_B] or V outside [2, MDSS_MAX_V]; a size of the cache or beam
+                            calls outside its range */
   MDSS_EUNSUPPORTED = 3, /* K outside {2, 3} for mdss_induced_dist, outside [2, MDSS_MAX_K] for
                             the selection and the exponential-sum calls (MDSS_SUCCESSIVE_MAX_K for
                             the successive calls), K = 3 with s_max outside [1, MDSS_K3_MAX_SUPPORT],
@@ -497,6 +498,156 @@ mdss_status mdss_select_truncated_lp(const float* p, const float* q1, const floa
                                      const float* u, uint64_t seed, uint64_t offset, int64_t B, int64_t V, int32_t s,
                                      int32_t tail, const int32_t* omega1, const double* w, int32_t* sel_index,
                                      int32_t* sel_token, int32_t* row_status, void* stream);
+
+/* ---- Paged cache of keys and values in 8 bits ------------------------------
+ * What a decoding loop with several hypotheses keeps between its steps: the
+ * drafts of a speculative step, or the beams of a search, share the pages of
+ * their common past and own the rest.
+ *
+ * A pool holds `pages` pages for every layer; a page is page_size tokens of
+ * every head, in units of 16 tokens:
+ *   k      [layers][pages][heads][page_size / 16][head_dim / 16][16 tokens][16 of head_dim]  e4m3 codes
+ *   v      [layers][pages][heads][page_size / 16][head_dim][16 tokens]                       e4m3 codes
+ *   k_exp, v_exp [layers][pages][heads] int8
+ * A value is code * 2^exp: one exponent for the block of tokens that a page
+ * is, and a head; exponents lie in [MDSS_CACHE_MIN_EXP, MDSS_CACHE_MAX_EXP].
+ * (Each unit holds 16 bytes together for the lane of the matrix product that
+ * wants them, keys by token and values by element.)  k and v are 16-byte aligned.
+ *
+ * A sequence is a row of `table` ([S][width] int32 page ids, -1 where there is
+ * none) and a length: its tokens 0 .. length - 1 lie in pages
+ * table[s][t / page_size].  refs [pages] int32 counts the rows that hold a page;
+ * 0 is a free page.  Tables, lengths and refs are the caller's; the calls keep
+ * nothing.  Row status bit MDSS_ROW_NO_PAGE (64), OR-ed: the row has no page for
+ * what it was asked to hold.  A page id outside [0, pages) is never followed.
+ *
+ * New tokens come ragged: sequence s owns tokens starts[s] .. starts[s + 1] - 1
+ * (starts [S + 1] int32, ascending from 0 to at most T; NULL: T / S tokens each,
+ * T a multiple of S), which are the last of its lengths[s] tokens.
+ *
+ * Sizes (else MDSS_ESHAPE): layers in [1, 65535], pages in [1, 2^24], heads in
+ * [1, 1024], T in [0, 2^24], S in [0, MDSS_MAX_B], width >= 1, S * width < 2^31;
+ * page_size 16, 32, 64, 128 or 256 and head_dim 64, 96, 128 or 256 (else
+ * MDSS_EUNSUPPORTED).  S = 0 or T = 0: nothing to do, MDSS_OK. */
+#define MDSS_ROW_NO_PAGE 64
+#define MDSS_CACHE_MIN_EXP (-40)
+#define MDSS_CACHE_MAX_EXP 40
+
+typedef enum mdss_dtype { MDSS_F32 = 0, MDSS_BF16 = 1, MDSS_F16 = 2 } mdss_dtype;
+
+typedef struct mdss_cache {
+  uint8_t* k;      /* device pointers */
+  uint8_t* v;
+  int8_t* k_exp;
+  int8_t* v_exp;
+  int64_t pages;
+  int32_t layers, heads, head_dim, page_size;
+} mdss_cache;      /* a host struct, read during the call */
+
+/* Writes new keys and values ([T][heads][head_dim], MDSS_BF16 or MDSS_F16; the
+ * last dimension contiguous, the others by strides in elements) into `layer`.
+ * For each page and head with a = the largest finite magnitude of its new tokens:
+ * e = the least exponent with a <= 448 * 2^e, clamped to the range, and not below
+ * the page's own exponent if the page holds earlier tokens of the sequence; those
+ * go to the new exponent (code * 2^(old - e), rounded to the nearest code, ties to
+ * even).  New codes are x * 2^-e, rounded so (beyond 448, which a clamped exponent
+ * allows: 448); NaN and infinities become the NaN code with their sign.
+ * lengths include the new tokens.  The pages written must not be held by
+ * another row (mdss_cache_fork sees to it).  A row whose tokens do not fit the
+ * table or whose page id is out of range is flagged; such pages are not written. */
+mdss_status mdss_cache_append(const mdss_cache* cache, int32_t layer, const void* key, int64_t key_token_stride,
+                              int64_t key_head_stride, const void* value, int64_t value_token_stride,
+                              int64_t value_head_stride, mdss_dtype dtype, int64_t T, const int32_t* starts,
+                              const int32_t* table, int64_t width, const int32_t* lengths, int64_t S,
+                              int32_t* row_status, void* stream);
+
+/* Attention of the new tokens over their sequences' cached ones: for query i (of
+ * n) of sequence s, at position lengths[s] - n + i, and query head hq, which
+ * reads cache head hq / (heads_q / heads):
+ *   out = sum_j softmax_j(scale * q . k_j) v_j over the tokens j up to its own.
+ * q [T][heads_q][head_dim] MDSS_BF16 or MDSS_F16 (token and head strides in
+ * elements, last dimension contiguous); out [T][heads_q][head_dim] of the same
+ * type, contiguous, 16-byte aligned; lse (nullable) [T][heads_q] fp32: the natural log of the sum
+ * of exp(scale q . k_j).  A row that sees no token (position < 0, no page) gets
+ * 0 and -inf; tokens of T that belong to no sequence are not written.  Bytes past
+ * a sequence's tokens are never seen, whatever they hold, and a NaN in a key or
+ * value reaches only the rows that see its token.  Products are of bf16 or f16 (q's
+ * type; values and weights f16) with sums, maxima and normalisers in fp32.
+ * max_new and max_length are host-side hints (0: none) on the most new tokens and the largest length
+ * of a sequence; they choose how the work is cut and never the result's tokens.
+ * heads_q: a multiple of heads, at most 1024 per head, T * heads_q < 2^31.  workspace: at least
+ * mdss_workspace_bytes_attention(...) bytes, 256-byte aligned (may be NULL if
+ * that is 0). */
+size_t mdss_workspace_bytes_attention(const mdss_cache* cache, int64_t T, int64_t S, int64_t width, int64_t heads_q,
+                                      int32_t uniform, int64_t max_new, int64_t max_length);
+mdss_status mdss_cache_attention(const mdss_cache* cache, int32_t layer, const void* q, int64_t q_token_stride,
+                                 int64_t q_head_stride, mdss_dtype dtype, int64_t T, int64_t heads_q,
+                                 const int32_t* starts, const int32_t* table, int64_t width, const int32_t* lengths,
+                                 int64_t S, float scale, int64_t max_new, int64_t max_length, void* out, float* lse,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Replaces rows by their parents' (beam reordering, drafts branching, the kept
+ * draft, freeing) and makes room for the tokens to come, in one call:
+ *   - row i of the S_out rows that go out holds the first len = min(lengths[parent[i]],
+ *     keep[i]) tokens of row parent[i] (parent NULL: row i, and S_out <= S; outside [0, S): no
+ *     tokens; keep NULL: all).  refs loses what the S rows held and gains what
+ *     the S_out rows hold; a page that nobody holds is free from the next call on.
+ *   - grow[i] (nullable) more tokens: the row gets the pages for len + grow[i], and a
+ *     partly filled last page that other rows hold too is replaced by a copy, in all
+ *     layers (of several rows that grow on one page, the highest keeps it if no other row holds it).
+ *     Pages are the lowest-numbered ones with refs = 0 on entry, handed out by
+ *     ascending row (the copy first).
+ *   - lengths_out[i] = len + grow[i]; table_out row i: its pages, then -1.
+ * If the free pages do not suffice for all, no row grows and no page is copied
+ * (lengths_out = len): rows with grow > 0 are flagged.  A row whose growth passes
+ * the table's width does not grow and is flagged.
+ * refs_out may be refs; table_out must not be table, nor lengths_out lengths.  row_status [S_out]. */
+size_t mdss_workspace_bytes_cache_fork(const mdss_cache* cache, int64_t S_out);
+mdss_status mdss_cache_fork(const mdss_cache* cache, const int32_t* table, const int32_t* lengths, int64_t S,
+                            int64_t width, const int32_t* refs, const int32_t* parent, const int32_t* keep,
+                            const int32_t* grow, int64_t S_out, int32_t* table_out, int32_t* lengths_out,
+                            int32_t* refs_out, int32_t* row_status, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/* Moves the used pages to the ids 0 .. used - 1, in all layers: with U pages used,
+ * the r-th highest used page >= U goes to the r-th lowest free page < U.
+ * table_out (may be table): the rows with the new ids, -1 past a row's tokens;
+ * refs_out (not refs): the counts; used [1] int32: U. */
+size_t mdss_workspace_bytes_cache_compact(const mdss_cache* cache);
+mdss_status mdss_cache_compact(const mdss_cache* cache, const int32_t* table, const int32_t* lengths, int64_t S,
+                               int64_t width, const int32_t* refs, int32_t* table_out, int32_t* refs_out,
+                               int32_t* used, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Copies pages src[i] to dst[i] (i < n), codes and exponents, in all layers.  No
+ * page may be written twice or be both a source and a destination; pairs with an id out of
+ * range are left out. */
+mdss_status mdss_cache_copy(const mdss_cache* cache, const int32_t* src, const int32_t* dst, int64_t n, void* stream);
+
+/* ---- Beam search ------------------------------------------------------------
+ * logits [B][W][V] (any mdss_dtype; rows contiguous, row_stride elements apart),
+ * scores [B][W] fp32.  A candidate (w, v) has
+ *   total = ((x_v - m) - log sum_j exp(x_j - m)) + scores[b][w],  m = max_j x_j, in fp32.
+ * The n best of a group b, by the larger total, then the lower beam, then the
+ * larger logit, then the lower token: parent [B][n] (the beam), token, score_out
+ * (the total).  A beam with done[b][w] (nullable) has one candidate, the token eos with
+ * its own score, and its logits are not read; a beam whose score is not finite has
+ * none, nor have tokens of logit or total -inf.  A beam with a NaN or +inf logit has none and
+ * row_status[b * W + w] gets MDSS_ROW_BAD_PROB.  Places without a candidate: parent
+ * and token -1, score -inf, done 0.  done_out [B][n]: the parent's done, or token = eos
+ * (eos -1: no such token).
+ * B * W and B * n up to 65535, W and n in [1, MDSS_MAX_BEAMS], V in [1, MDSS_MAX_V].
+ * workspace: at least mdss_workspace_bytes_beam(B, W, V, n) bytes, 256-byte aligned. */
+#define MDSS_MAX_BEAMS 64
+size_t mdss_workspace_bytes_beam(int64_t B, int64_t W, int64_t V, int64_t n);
+mdss_status mdss_beam_select(const void* logits, mdss_dtype dtype, int64_t row_stride, const float* scores,
+                             const uint8_t* done, int64_t B, int64_t W, int64_t V, int64_t n, int32_t eos,
+                             int32_t* parent, int32_t* token, float* score_out, uint8_t* done_out,
+                             int32_t* row_status, void* workspace, size_t workspace_bytes, void* stream);
+
+/* out [B][n] rows of row_bytes bytes: out[b][j] = state[b][parent[b][j]] (state
+ * [B][W] rows), zeros where the parent is outside [0, W).  out must not overlap state. */
+mdss_status mdss_beam_reorder(const void* state, const int32_t* parent, int64_t B, int64_t W, int64_t n,
+                              int64_t row_bytes, void* out, void* stream);
 
 /* Static, thread-safe description of a status code. */
 const char* mdss_status_string(mdss_status s);

@@ -17,6 +17,8 @@ Contents:
   * ``tlp.py``         -- numpy/scipy: the truncated linear program (Algorithm 2,
     its sort-free variant and the two-distribution version), its LP solved by
     HiGHS in the paper's own variables.
+  * ``cache.py``       -- numpy: the paged 8-bit cache (rounding, append, attention, fork, compact).
+  * ``beam.py``        -- numpy: the beam step.
 
 Notation: ``p`` = TARGET, ``q`` = DRAFT (the paper uses the opposite letters).
 """

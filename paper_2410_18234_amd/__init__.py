@@ -16,9 +16,13 @@ from .binding import (  # noqa: F401
     MDSS_ROW_FORCED,
     MDSS_ROW_LP_LIMIT,
     MDSS_ROW_RANGE,
+    MDSS_CACHE_MAX_EXP,
+    MDSS_CACHE_MIN_EXP,
+    MDSS_MAX_BEAMS,
     MDSS_MAX_K,
     MDSS_NOALLOC_SCRATCH_BYTES,
     MDSS_OPTIMUM_MAX_K,
+    MDSS_ROW_NO_PAGE,
     MDSS_ROW_SUPPORT,
     MDSS_SUCCESSIVE_MAX_K,
     MDSS_TLP_HALF,
@@ -64,4 +68,16 @@ from .binding import (  # noqa: F401
     workspace_bytes_pair,
     workspace_bytes_successive,
     workspace_bytes_tlp,
+)
+from .beam import (  # noqa: F401
+    beam_reorder,
+    beam_select,
+)
+from .cache import (  # noqa: F401
+    PagedCache,
+    cache_append,
+    cache_attention,
+    cache_compact,
+    cache_copy,
+    cache_fork,
 )

@@ -29,6 +29,10 @@ MDSS_TLP_SORTED = 0
 MDSS_TLP_HALF = 1
 MDSS_SUCCESSIVE_MAX_K = 8
 MDSS_OPTIMUM_MAX_K = 8
+MDSS_ROW_NO_PAGE = 64
+MDSS_CACHE_MIN_EXP = -40
+MDSS_CACHE_MAX_EXP = 40
+MDSS_MAX_BEAMS = 64
 
 _STATUS = {0: "MDSS_OK", 1: "MDSS_EINVAL", 2: "MDSS_ESHAPE", 3: "MDSS_EUNSUPPORTED", 4: "MDSS_EDEVICE",
            5: "MDSS_EWORKSPACE"}
@@ -102,6 +106,24 @@ def load_library():
         lib.mdss_induced_dist_topk_expsum_sums.argtypes = [P, P, i64, i64, i32, i32, P, P, P, sz, P]
         lib.mdss_step_topk_expsum.argtypes = [P, P, P, P, u64, u64, i64, i64, i32, i32, P, P, P, P, P, P, P, P, sz,
                                               P]
+        lib.mdss_cache_append.argtypes = [P, i32, P, i64, i64, P, i64, i64, i32, i64, P, P, i64, P, i64, P, P]
+        lib.mdss_workspace_bytes_attention.argtypes = [P, i64, i64, i64, i64, i32, i64, i64]
+        lib.mdss_cache_attention.argtypes = [P, i32, P, i64, i64, i32, i64, i64, P, P, i64, P, i64, ctypes.c_float, i64,
+                                             i64, P, P, P, sz, P]
+        lib.mdss_workspace_bytes_cache_fork.argtypes = [P, i64]
+        lib.mdss_cache_fork.argtypes = [P, P, P, i64, i64, P, P, P, P, i64, P, P, P, P, P, sz, P]
+        lib.mdss_workspace_bytes_cache_compact.argtypes = [P]
+        lib.mdss_cache_compact.argtypes = [P, P, P, i64, i64, P, P, P, P, P, sz, P]
+        lib.mdss_cache_copy.argtypes = [P, P, P, i64, P]
+        lib.mdss_workspace_bytes_beam.argtypes = [i64, i64, i64, i64]
+        lib.mdss_beam_select.argtypes = [P, i32, i64, P, P, i64, i64, i64, i64, i32, P, P, P, P, P, P, sz, P]
+        lib.mdss_beam_reorder.argtypes = [P, P, i64, i64, i64, i64, P, P]
+        for f in ("mdss_workspace_bytes_attention", "mdss_workspace_bytes_cache_fork",
+                  "mdss_workspace_bytes_cache_compact", "mdss_workspace_bytes_beam"):
+            getattr(lib, f).restype = sz
+        for f in ("mdss_cache_append", "mdss_cache_attention", "mdss_cache_fork", "mdss_cache_compact",
+                  "mdss_cache_copy", "mdss_beam_select", "mdss_beam_reorder"):
+            getattr(lib, f).restype = ctypes.c_int
         for f in ("mdss_induced_dist_successive", "mdss_select_successive", "mdss_optimal_acceptance",
                   "mdss_acceptance", "mdss_induced_dist_expsum", "mdss_induced_dist_pair_expsum",
                   "mdss_induced_dist_successive_expsum", "mdss_induced_dist_expsum_noalloc",
