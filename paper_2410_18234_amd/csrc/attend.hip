@@ -11,7 +11,7 @@
 // waves of a workgroup at the end.  One pass with a running maximum: with t = s log2(e) + ve, in the frame M = max t,
 //   p = 2^(t - M) <= 1 carries the value's scale (so f16 holds the terms that matter, whatever the pages' scales),
 //   l = sum p 2^-ve the softmax's sum in the same frame, out = sum p code / l.
-// Exponents lie in [-40, 40]: a term that the frame loses (below 2^-126) has less than 2^-46 of the largest weight.
+// (c_g = scale log2(e) 2^ke is the lane's, so t is one fused multiply-add.)  Exponents lie in [-40, 40]: a term that the frame loses (below 2^-126) has less than 2^-46 of the largest weight.
 #include "cache.h"
 
 #include <math.h>
@@ -38,7 +38,8 @@ struct AttendArgs {
   int S, heads, group, page_shift;
   int per_seq;   // row tiles of a sequence (uniform), 0: found from starts
   int splits, split_tiles;
-  float scale_log2;
+  float scale_log2;  // |scale| log2(e)
+  bool negative;
 };
 
 template <bool BF>
@@ -111,84 +112,215 @@ __device__ __forceinline__ u32x4 low_bytes(u32x4 x, int keep) {
 // The frame of two partial sums: their weights, given (M, l) of each; rows without a visible token have M = -inf.
 __device__ __forceinline__ float frame_weight(float M, float top) { return M == -INFINITY ? 0.0f : exp2f(M - top); }
 
-// WIDE: the four waves of a workgroup take different rows of the same tokens (many rows); else the same rows of
-// different tokens, joined at the end.
-template <int D, bool BF, int MT, bool WIDE>
-__global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
-  using E = Elem<BF>;
-  using vec = typename E::vec;
-  using one = typename E::one;
-  constexpr int kSteps = D / 32;             // matrix steps over d
-  constexpr int kWhole = D / 64;             // 16-byte loads of a key row's quarter
-  constexpr bool kHalf = D % 64 != 0;        // and one of 8 bytes
-  constexpr int kTiles = D / 16;             // accumulator tiles over d
-  constexpr int kRows = (WIDE ? 64 : 16) * MT;
-  constexpr int kPad = D + 4;
-  __shared__ __align__(16) float joined[WIDE ? 1 : 4 * 16 * kPad];
-  __shared__ float joined_ml[WIDE ? 1 : 4 * 16 * 2];
+// The pages of a sequence's units, never out of the table or the pool.
+struct PageWalk {
+  const int32_t* row;
+  int64_t pages;
+  int heads, h, unit_shift, last_page;  // (a page has 1 << unit_shift units)
+  __device__ __forceinline__ PageWalk(const AttendArgs& a, const struct Place& p);
+  __device__ __forceinline__ int page(int unit) const { return row[min(unit >> unit_shift, last_page)]; }
+  __device__ __forceinline__ int valid(int page, bool& ok) const {  // page 0 in place of none
+    ok = (uint32_t)page < (uint64_t)pages;
+    return ok ? page : 0;
+  }
+  __device__ __forceinline__ const uint8_t* unit(const uint8_t* base, int page, int unit, int bytes) const {
+    return base + ((((int64_t)page * heads + h) << unit_shift) + (unit & ((1 << unit_shift) - 1))) * bytes;
+  }
+};
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-  // the head is the fastest index: the row tiles that read one head's pages run on the same XCD where heads are a
-  // multiple of 8 (workgroups go round the XCDs in order), and find them in its L2
-  const int slot = blockIdx.x / a.heads, h = blockIdx.x - slot * a.heads, split = blockIdx.y;
-  int s, tile;
-  int64_t start;
-  int n;
+// Where a workgroup stands: its row tile of a sequence, and what that sequence holds.
+struct Place {
+  int s, tile, h;
+  int n, rows;      // new tokens, and rows (tokens x query heads of this cache head)
+  int64_t start;    // its first token of T
+  int len, before;  // cached tokens (as far as the table goes); those before the new ones (negative: the first rows see nothing)
+};
+// The head is the fastest index of the grid: the row tiles that read one head's pages run on the same XCD where heads
+// are a multiple of 8 (workgroups go round the XCDs in order), and find them in its L2.
+__device__ __forceinline__ bool attend_place(const AttendArgs& a, int tile_rows, int lane, Place& p) {
+  const int slot = blockIdx.x / a.heads;
+  p.h = blockIdx.x - slot * a.heads;
   if (a.per_seq > 0) {
-    s = slot / a.per_seq;
-    tile = slot - s * a.per_seq;
+    p.s = slot / a.per_seq;
+    p.tile = slot - p.s * a.per_seq;
   } else {
-    s = slot_sequence(a.starts, a.S, slot, a.group, kRows, 1, lane);
-    tile = slot - (int)slot_first(a.starts, s, a.group, kRows, 1);
+    p.s = slot_sequence(a.starts, a.S, slot, a.group, tile_rows, 1, lane);
+    p.tile = slot - (int)slot_first(a.starts, p.s, a.group, tile_rows, 1);
   }
   if (a.starts) {
-    start = a.starts[s];
-    n = (int)(a.starts[s + 1] - start);
+    p.start = a.starts[p.s];
+    p.n = (int)(a.starts[p.s + 1] - p.start);
   } else {
-    n = (int)(a.T / a.S);
-    start = (int64_t)s * n;
+    p.n = (int)(a.T / a.S);
+    p.start = (int64_t)p.s * p.n;
   }
-  if (start < 0 || n <= 0 || start + n > a.T) return;  // no rows, or starts that are not ascending within T
-  const int rows = n * a.group;
-  if (tile * kRows >= rows) return;
-  const int row0 = tile * kRows + (WIDE ? wave * 16 * MT : 0);
-  if (row0 >= rows) return;  // (WIDE only: the wave has no row, and there is no barrier below)
-  const int len = max(0, min(a.lengths[s], (int)min(a.width << a.page_shift, (int64_t)INT32_MAX)));
-  const int before = a.lengths[s] - n;  // tokens cached before the new ones (negative: the first rows see nothing)
-  const int lim_lo = min(len, before + row0 / a.group + 1);
-  const int lim_hi = min(len, before + min(rows - 1, row0 + 16 * MT - 1) / a.group + 1);
-  const int tiles = lim_hi > 0 ? (lim_hi + 63) >> 6 : 0;
-  const int t_begin = split * a.split_tiles;
-  const int t_end = split == a.splits - 1 ? tiles : min(tiles, t_begin + a.split_tiles);
-  // a split without tokens for any row of the workgroup has nothing to say (the first one always speaks)
-  if (split > 0 && t_begin >= tiles) return;
+  if (p.start < 0 || p.n <= 0 || p.start + p.n > a.T) return false;  // no rows, or starts that do not ascend within T
+  p.rows = p.n * a.group;
+  if (p.tile * tile_rows >= p.rows) return false;
+  const int length = a.lengths[p.s];
+  p.len = max(0, min(length, (int)min(a.width << a.page_shift, (int64_t)INT32_MAX)));
+  p.before = length - p.n;
+  return true;
+}
+// Tokens that the rows up to `last` see at most.
+__device__ __forceinline__ int seen_by(const AttendArgs& a, const Place& p, int last) {
+  return min(p.len, p.before + min(p.rows - 1, last) / a.group + 1);
+}
 
-  // queries: lane (m, g) holds row m's elements 64 i + 16 g + 0..15 (8 g' of the last 32 where D is no multiple of 64)
-  vec qf[MT][kSteps];
-  int lim[MT];
+__device__ __forceinline__ PageWalk::PageWalk(const AttendArgs& a, const Place& p)
+    : row(a.table + (int64_t)p.s * a.width), pages(a.pages), heads(a.heads), h(p.h), unit_shift(a.page_shift - 4),
+      last_page(p.len > 0 ? (p.len - 1) >> a.page_shift : 0) {}
+
+// Row r's queries: lane (m, g) holds elements 64 i + 16 g + 0 .. 15 (the last 32 of a D that is no multiple of 64: 8 g ..),
+// negated where the scale is negative, so that a larger product is a larger score.
+template <int D, bool BF, int MT>
+__device__ __forceinline__ void load_queries(const AttendArgs& a, const Place& p, int row0, int m, int g,
+                                             typename Elem<BF>::vec (&qf)[MT][D / 32], int (&lim)[MT]) {
+  typedef typename Elem<BF>::vec vec;
+  typedef typename Elem<BF>::one one;
 #pragma unroll
   for (int r = 0; r < MT; ++r) {
     const int row = row0 + 16 * r + m;
-    const bool in = row < rows;
+    const bool in = row < p.rows;
     const int i = in ? row / a.group : 0, hg = in ? row - i * a.group : 0;
-    lim[r] = in ? min(len, before + i + 1) : 0;
-    const one* qr = static_cast<const one*>(a.q) + (start + i) * a.q_st + (int64_t)(h * a.group + hg) * a.q_sh;
+    lim[r] = in ? min(p.len, p.before + i + 1) : 0;
+    const one* qr = static_cast<const one*>(a.q) + (p.start + i) * a.q_st + (int64_t)(p.h * a.group + hg) * a.q_sh;
 #pragma unroll
-    for (int st = 0; st < kSteps; ++st) {
-      const int at = (kHalf && st == kSteps - 1) ? 64 * kWhole + 8 * g : 64 * (st >> 1) + 16 * g + 8 * (st & 1);
+    for (int st = 0; st < D / 32; ++st) {
+      const int at = (D % 64 != 0 && st == D / 32 - 1) ? D - 32 + 8 * g : 64 * (st >> 1) + 16 * g + 8 * (st & 1);
       vec x;
-      if (((reinterpret_cast<uintptr_t>(qr) & 15) == 0)) {
+      if ((reinterpret_cast<uintptr_t>(qr) & 15) == 0) {
         x = *reinterpret_cast<const vec*>(qr + at);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = qr[at + j];
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = in ? x[j] : (one)0.0f;
+      for (int j = 0; j < 8; ++j) x[j] = !in ? (one)0.0f : a.negative ? -x[j] : x[j];
       qf[r][st] = x;
     }
   }
+}
 
+// The weights of 64 tokens from their scores: p = 2^(t - M) in f16, the normaliser, and by how much what was summed before
+// shrinks (returns whether it does).  All of a lane's scores are of one unit, so its page's scales are one factor
+// and one addend (c_g >= 0, ve_g), and the maximum can be taken of the products themselves.  M follows the maximum
+// only when some row's has grown by more than 2^kSlack: p stays far inside f16, and the sums are rescaled once or twice in
+// all instead of whenever one of the rows finds a larger score.  upto[r]: the unit's tokens that row r sees.
+constexpr float kSlack = 8.0f;
+template <int MT, bool MASKED>
+__device__ __forceinline__ bool weigh(const f32x4 (&sc)[4][MT], float c_g, float ve_g, float inv_v, const int (&upto)[MT],
+                                      float (&M)[MT], float (&l)[MT], float (&alpha)[MT], f16x8 (&pf)[MT][2]) {
+  float top[MT];
+  bool grown = false;
+#pragma unroll
+  for (int r = 0; r < MT; ++r) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, !MASKED || 4 * tt + i < upto[r] ? sc[tt][r][i] : -INFINITY);
+    top[r] = row_max4(mx == -INFINITY ? mx : fmaf(mx, c_g, ve_g));
+    grown |= top[r] > M[r] + kSlack;
+  }
+  grown = __ballot(grown) != 0;
+  if (grown) {
+#pragma unroll
+    for (int r = 0; r < MT; ++r) {
+      const float to = fmaxf(M[r], top[r]);
+      alpha[r] = M[r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M[r] - to);
+      l[r] *= alpha[r];
+      M[r] = to;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < MT; ++r) {
+    const float off = ve_g - (M[r] == -INFINITY ? 0.0f : M[r]);
+    float sum = 0.0f;
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float p = __builtin_amdgcn_exp2f(fmaf(sc[tt][r][i], c_g, off));
+        if (MASKED) p = 4 * tt + i < upto[r] ? p : 0.0f;
+        sum += p;
+        pf[r][tt >> 1][4 * (tt & 1) + i] = (_Float16)p;
+      }
+    l[r] = fmaf(sum, inv_v, l[r]);
+  }
+  return grown;
+}
+
+// A NaN code among tokens that only some rows see must reach those rows alone: it is taken out of the values (a lane's 16
+// tokens of one d) and counted in a product of its own.
+__device__ __forceinline__ uint32_t nan_any(const u32x4& v) {
+  return nan_bytes(v[0]) | nan_bytes(v[1]) | nan_bytes(v[2]) | nan_bytes(v[3]);
+}
+__device__ __forceinline__ u32x4 nan_out(u32x4 v) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) v[w] &= ~((nan_bytes(v[w]) >> 7) * 0xffu);
+  return v;
+}
+template <int MT>
+__device__ __forceinline__ void mark_nan(const u32x4& v, const int (&upto)[MT], f32x4 (&acc)[MT]) {
+  u32x4 flag;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) flag[w] = (nan_bytes(v[w]) >> 7) * 0x38u;  // the code of 1.0
+#pragma unroll
+  for (int r = 0; r < MT; ++r) {
+    f32x4 hit = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int hs = 0; hs < 2; ++hs) {
+      f16x8 see;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) see[j] = 8 * hs + j < upto[r] ? (_Float16)1.0f : (_Float16)0.0f;
+      hit = Elem<false>::mfma(Elem<false>::widen(flag[2 * hs], flag[2 * hs + 1]), see, hit);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[r][i] = hit[i] > 0.0f ? NAN : acc[r][i];
+  }
+}
+
+template <int MT>
+__device__ __forceinline__ void add_values(const f16x8 (&v)[2], const f16x8 (&pf)[MT][2], f32x4 (&acc)[MT]) {
+#pragma unroll
+  for (int hs = 0; hs < 2; ++hs)
+#pragma unroll
+    for (int r = 0; r < MT; ++r) acc[r] = Elem<false>::mfma(v[hs], pf[r][hs], acc[r]);
+}
+
+// Few rows: the four waves of a workgroup take the same rows against tiles of 64 tokens in turn, straight from memory
+// to registers, and join at the end.  Bound by memory: a tile's keys are loaded while the one before is
+// weighed, its values while its keys are multiplied.
+template <int D, bool BF, int MT>
+__global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
+  using E = Elem<BF>;
+  using vec = typename E::vec;
+  using one = typename E::one;
+  constexpr int kSteps = D / 32;       // matrix steps over d
+  constexpr int kWhole = D / 64;       // 16-byte loads of a key's quarter
+  constexpr bool kHalf = D % 64 != 0;  // and one of 8 bytes
+  constexpr int kTiles = D / 16;       // accumulator tiles over d
+  constexpr int kPad = D + 4;
+  __shared__ __align__(16) float joined[4 * 16 * kPad];
+  __shared__ float joined_ml[4 * 16 * 2];
+
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int split = blockIdx.y;
+  Place p;
+  if (!attend_place(a, 16 * MT, lane, p)) return;
+  const int row0 = p.tile * 16 * MT, h = p.h;
+  const int lim_lo = seen_by(a, p, row0), lim_hi = seen_by(a, p, row0 + 16 * MT - 1);
+  const int tiles = lim_hi > 0 ? (lim_hi + 63) >> 6 : 0;
+  const int t_begin = split * a.split_tiles;
+  const int t_end = split == a.splits - 1 ? tiles : min(tiles, t_begin + a.split_tiles);
+  // a split without tokens for any of the rows has nothing to say (the first one always speaks)
+  if (split > 0 && t_begin >= tiles) return;
+
+  vec qf[MT][kSteps];
+  int lim[MT];
+  load_queries<D, BF, MT>(a, p, row0, m, g, qf, lim);
   f32x4 acc[kTiles][MT];
   float M[MT], l[MT];
 #pragma unroll
@@ -199,47 +331,32 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
     for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  const int step = WIDE ? 1 : 4;
-  const int t0 = t_begin + (WIDE ? 0 : wave);
-  const int32_t* trow = a.table + (int64_t)s * a.width;
-  const int unit_shift = a.page_shift - 4;
-  const int last_page = len > 0 ? (len - 1) >> a.page_shift : 0;
-  const int per_page = 1 << unit_shift;
-  const auto page_at = [&](int unit) {  // page id of a unit, clamped into the row: never out of the table
-    return trow[min(unit >> unit_shift, last_page)];
-  };
-  const auto unit_base = [&](const uint8_t* base, int page, int unit) {
-    return base + ((((int64_t)page * a.heads + h) << unit_shift) + (unit & (per_page - 1))) * (16 * D);
-  };
-
-  u32x4 kc[4][kWhole > 0 ? kWhole : 1];
+  const int t0 = t_begin + wave;
+  const PageWalk walk(a, p);
+  u32x4 kc[4][kWhole];
   u32x2 kh[4];
   const auto load_k = [&](int page, int t) {
-    const int unit = 4 * t + (m >> 2);
-    const uint8_t* p = unit_base(a.k, page, unit) + g * 256 + (m & 3) * 16;
+    const uint8_t* at = walk.unit(a.k, page, 4 * t + (m >> 2), 16 * D) + (m & 3) * 16;
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) {
 #pragma unroll
-      for (int i = 0; i < kWhole; ++i) kc[tt][i] = *reinterpret_cast<const u32x4*>(p + tt * 64 + i * 1024);
-      if (kHalf)
-        kh[tt] = *reinterpret_cast<const u32x2*>(p - g * 256 + (4 * kWhole + (g >> 1)) * 256 + (g & 1) * 8 + tt * 64);
+      for (int i = 0; i < kWhole; ++i) kc[tt][i] = *reinterpret_cast<const u32x4*>(at + tt * 64 + i * 1024 + g * 256);
+      if (kHalf) kh[tt] = *reinterpret_cast<const u32x2*>(at + tt * 64 + (4 * kWhole + (g >> 1)) * 256 + (g & 1) * 8);
     }
   };
 
   if (t0 < t_end) {
-    int pk = page_at(4 * t0 + (m >> 2)), pv = page_at(4 * t0 + g);
-    bool ok_k = (uint32_t)pk < (uint32_t)a.pages;
-    load_k(ok_k ? pk : 0, t0);
-    bool ok = (uint32_t)pv < (uint32_t)a.pages;
-    pv = ok ? pv : 0;
+    bool ok, ok_k;
+    int pk = walk.valid(walk.page(4 * t0 + (m >> 2)), ok_k), pv = walk.valid(walk.page(4 * t0 + g), ok);
+    load_k(pk, t0);
     int ke = a.k_exp[(int64_t)pv * a.heads + h], ve = a.v_exp[(int64_t)pv * a.heads + h];
-    int pk_next = page_at(4 * (t0 + step) + (m >> 2)), pv_next = page_at(4 * (t0 + step) + g);
-    for (int t = t0; t < t_end; t += step) {
+    int pk_next = walk.page(4 * (t0 + 4) + (m >> 2)), pv_next = walk.page(4 * (t0 + 4) + g);
+    for (int t = t0; t < t_end; t += 4) {
       u32x4 vc[kTiles];
       {
-        const uint8_t* p = unit_base(a.v, pv, 4 * t + g) + m * 16;
+        const uint8_t* at = walk.unit(a.v, pv, 4 * t + g, 16 * D) + m * 16;
 #pragma unroll
-        for (int dt = 0; dt < kTiles; ++dt) vc[dt] = *reinterpret_cast<const u32x4*>(p + dt * 256);
+        for (int dt = 0; dt < kTiles; ++dt) vc[dt] = *reinterpret_cast<const u32x4*>(at + dt * 256);
       }
       f32x4 sc[4][MT];
 #pragma unroll
@@ -257,152 +374,58 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
       const float c_g = a.scale_log2 * pow2i(ke), ve_g = (float)ve, inv_v = pow2i(-ve);
       const bool ok_now = ok;
       // the next tile's keys, exponents, and the page ids after it
-      {
-        const bool nk = (uint32_t)pk_next < (uint32_t)a.pages;
-        load_k(nk ? pk_next : 0, t + step);
-        ok = (uint32_t)pv_next < (uint32_t)a.pages;
-        pv = ok ? pv_next : 0;
-        ke = a.k_exp[(int64_t)pv * a.heads + h];
-        ve = a.v_exp[(int64_t)pv * a.heads + h];
-        pk_next = page_at(4 * (t + 2 * step) + (m >> 2));
-        pv_next = page_at(4 * (t + 2 * step) + g);
-      }
+      pk = walk.valid(pk_next, ok_k);
+      load_k(pk, t + 4);
+      pv = walk.valid(pv_next, ok);
+      ke = a.k_exp[(int64_t)pv * a.heads + h];
+      ve = a.v_exp[(int64_t)pv * a.heads + h];
+      pk_next = walk.page(4 * (t + 8) + (m >> 2));
+      pv_next = walk.page(4 * (t + 8) + g);
+
       const bool masked = 64 * (t + 1) > lim_lo || __ballot(ok_now) != ~0ull;
       const int first = 64 * t + 16 * g;  // the lane's first token
+      int upto[MT];
+#pragma unroll
+      for (int r = 0; r < MT; ++r) upto[r] = ok_now ? lim[r] - first : 0;
       f16x8 pf[MT][2];
-      bool grown = false;
       float alpha[MT];
-#pragma unroll
-      for (int r = 0; r < MT; ++r) {
-        float x[4][4], mx = -INFINITY;
-        if (masked) {
-          const int upto = ok_now ? lim[r] - first : 0;  // visible tokens of the unit
-#pragma unroll
-          for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              x[tt][i] = 4 * tt + i < upto ? fmaf(sc[tt][r][i], c_g, ve_g) : -INFINITY;
-              mx = fmaxf(mx, x[tt][i]);
-            }
-        } else {
-#pragma unroll
-          for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              x[tt][i] = fmaf(sc[tt][r][i], c_g, ve_g);
-              mx = fmaxf(mx, x[tt][i]);
-            }
-        }
-        const float top = fmaxf(M[r], row_max4(mx));
-        const float ref = top == -INFINITY ? 0.0f : top;
-        alpha[r] = __builtin_amdgcn_exp2f(M[r] - ref);
-        grown |= top > M[r];
-        M[r] = top;
-        float sum = 0.0f;
-#pragma unroll
-        for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p = __builtin_amdgcn_exp2f(x[tt][i] - ref);
-            sum += p;
-            pf[r][tt >> 1][4 * (tt & 1) + i] = (_Float16)p;
-          }
-        l[r] = fmaf(l[r], alpha[r], sum * inv_v);
-      }
-      if (__ballot(grown) != 0) {
+      const bool grown = masked ? weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, alpha, pf)
+                                : weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, alpha, pf);
+      if (grown) {
 #pragma unroll
         for (int r = 0; r < MT; ++r)
 #pragma unroll
           for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] *= alpha[r];
       }
       if (masked) {
-        // what lies past the sequence's end is not the cache's (any bytes), and a NaN code among the tokens that
-        // only some rows see must reach those rows alone: it is taken out here and counted in its own product
-        const int keep = ok_now ? min(max(len - first, 0), 16) : 0;
-        uint32_t bad = 0;
+        // what lies past the sequence's end is not the cache's: any bytes
+        const int keep = ok_now ? min(max(p.len - first, 0), 16) : 0;
+        uint32_t any = 0;
 #pragma unroll
         for (int dt = 0; dt < kTiles; ++dt) {
           vc[dt] = low_bytes(vc[dt], keep);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) bad |= nan_bytes(vc[dt][w]);
+          any |= nan_any(vc[dt]);
         }
-        if (__ballot(bad != 0) != 0) {
+        if (__ballot(any != 0) != 0) {
 #pragma unroll
           for (int dt = 0; dt < kTiles; ++dt) {
-            u32x4 flag;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const uint32_t b = nan_bytes(vc[dt][w]) >> 7;  // 0x01 in the bytes of NaN codes
-              flag[w] = b * 0x38u;                           // the code of 1.0
-              vc[dt][w] &= ~(b * 0xffu);
-            }
-#pragma unroll
-            for (int r = 0; r < MT; ++r) {
-              const int upto = ok_now ? lim[r] - first : 0;
-              f32x4 hit = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-              for (int hs = 0; hs < 2; ++hs) {
-                f16x8 see;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) see[j] = 8 * hs + j < upto ? (_Float16)1.0f : (_Float16)0.0f;
-                hit = Elem<false>::mfma(Elem<false>::widen(flag[2 * hs], flag[2 * hs + 1]), see, hit);
-              }
-#pragma unroll
-              for (int i = 0; i < 4; ++i) acc[dt][r][i] = hit[i] > 0.0f ? NAN : acc[dt][r][i];
-            }
+            mark_nan<MT>(vc[dt], upto, acc[dt]);
+            vc[dt] = nan_out(vc[dt]);
           }
         }
       }
 #pragma unroll
-      for (int dt = 0; dt < kTiles; ++dt)
-#pragma unroll
-        for (int hs = 0; hs < 2; ++hs) {
-          const f16x8 vf = Elem<false>::widen(vc[dt][2 * hs], vc[dt][2 * hs + 1]);
-#pragma unroll
-          for (int r = 0; r < MT; ++r) acc[dt][r] = Elem<false>::mfma(vf, pf[r][hs], acc[dt][r]);
-        }
-    }
-  }
-
-  const int64_t heads_q = (int64_t)a.heads * a.group;
-  const auto row_id = [&](int row) {  // row of [T][heads_q]
-    const int i = row / a.group;
-    return (start + i) * heads_q + h * a.group + (row - i * a.group);
-  };
-#pragma unroll
-  for (int r = 0; r < MT; ++r) l[r] = row_sum4(l[r]);
-
-  if (WIDE) {
-#pragma unroll
-    for (int r = 0; r < MT; ++r) {
-      const int row = row0 + 16 * r + m;
-      if (row >= rows) continue;
-      const int64_t id = row_id(row);
-      if (a.splits == 1) {
-        const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
-        one* o = static_cast<one*>(a.out) + id * D + 4 * g;
-#pragma unroll
-        for (int dt = 0; dt < kTiles; ++dt) {
-          typedef one one4 __attribute__((ext_vector_type(4)));
-          one4 w;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = (one)(l[r] == 0.0f ? 0.0f : acc[dt][r][i] * inv);
-          *reinterpret_cast<one4*>(o + 16 * dt) = w;
-        }
-        if (a.lse && g == 0) a.lse[id] = l[r] == 0.0f ? -INFINITY : (M[r] + log2f(l[r])) * 0.693147180559945f;
-      } else {
-        float* o = a.part + (id * a.splits + split) * D + 4 * g;
-#pragma unroll
-        for (int dt = 0; dt < kTiles; ++dt) *reinterpret_cast<f32x4*>(o + 16 * dt) = acc[dt][r];
-        if (g == 0) {
-          a.part_ml[2 * (id * a.splits + split)] = M[r];
-          a.part_ml[2 * (id * a.splits + split) + 1] = l[r];
-        }
+      for (int dt = 0; dt < kTiles; ++dt) {
+        const f16x8 v[2] = {Elem<false>::widen(vc[dt][0], vc[dt][1]), Elem<false>::widen(vc[dt][2], vc[dt][3])};
+        add_values<MT>(v, pf, acc[dt]);
       }
     }
-    return;
   }
+
   // join the four waves, 16 rows at a time: thread -> a row and D / 16 of its elements
+#pragma unroll
+  for (int r = 0; r < MT; ++r) l[r] = row_sum4(l[r]);
+  const int64_t heads_q = (int64_t)a.heads * a.group;
   const int jr = threadIdx.x >> 4, jd = (threadIdx.x & 15) * (D / 16);
 #pragma unroll
   for (int r = 0; r < MT; ++r) {
@@ -424,21 +447,22 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
       lsum = fmaf(wgt[i], joined_ml[(i * 16 + jr) * 2 + 1], lsum);
     }
     const int row = row0 + 16 * r + jr;
-    if (row < rows) {
-      const int64_t id = row_id(row);
+    if (row < p.rows) {
+      const int i = row / a.group;
+      const int64_t id = (p.start + i) * heads_q + h * a.group + (row - i * a.group);  // row of [T][heads_q]
       const float inv = lsum == 0.0f ? 0.0f : 1.0f / lsum;
 #pragma unroll
       for (int e = 0; e < D / 16; e += 2) {
         f32x2 o = {0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x2 x = *reinterpret_cast<const f32x2*>(joined + (i * 16 + jr) * kPad + jd + e);
-          o[0] = fmaf(wgt[i], x[0], o[0]);
-          o[1] = fmaf(wgt[i], x[1], o[1]);
+        for (int w4 = 0; w4 < 4; ++w4) {
+          const f32x2 x = *reinterpret_cast<const f32x2*>(joined + (w4 * 16 + jr) * kPad + jd + e);
+          o[0] = fmaf(wgt[w4], x[0], o[0]);
+          o[1] = fmaf(wgt[w4], x[1], o[1]);
         }
         if (a.splits == 1) {
           typedef one one2 __attribute__((ext_vector_type(2)));
-          one2 w2 = {(one)(lsum == 0.0f ? 0.0f : o[0] * inv), (one)(lsum == 0.0f ? 0.0f : o[1] * inv)};
+          const one2 w2 = {(one)(lsum == 0.0f ? 0.0f : o[0] * inv), (one)(lsum == 0.0f ? 0.0f : o[1] * inv)};
           *reinterpret_cast<one2*>(static_cast<one*>(a.out) + id * D + jd + e) = w2;
         } else {
           *reinterpret_cast<f32x2*>(a.part + (id * a.splits + split) * D + jd + e) = o;
@@ -451,6 +475,215 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
           a.part_ml[2 * (id * a.splits + split)] = top;
           a.part_ml[2 * (id * a.splits + split) + 1] = lsum;
         }
+      }
+    }
+  }
+}
+
+// Many rows: the four waves take different rows (MT tiles of 16 each) against the same tiles of 64 tokens, which go through
+// LDS: the next tile's codes are loaded while this one is multiplied, widened once for all four waves, and written for
+// the step after.  A piece of LDS is what one lane multiplies at a time (16 bytes), in the order of the lanes.
+template <int D, bool BF, int MT>
+__global__ __launch_bounds__(256, 2) void attend_wide_kernel(const AttendArgs a) {
+  using E = Elem<BF>;
+  using vec = typename E::vec;
+  using one = typename E::one;
+  constexpr int kSteps = D / 32, kWhole = D / 64, kTiles = D / 16;
+  constexpr bool kHalf = D % 64 != 0;
+  constexpr int kKeys = 4 * kWhole, kGroups = kKeys + kTiles;  // a lane's 16 codes: of keys (tt, i), then of values (dt)
+  constexpr int kEach = (kGroups + 3) / 4;                     // a wave loads these
+  constexpr int kKeyVecs = 4 * kSteps;                         // widened: keys (tt, step), then values (dt, half)
+  constexpr int kBuffers = D <= 128 ? 2 : 1;                   // (two workgroups a CU fit its 160 KB)
+  __shared__ __align__(16) vec key_tile[kBuffers][kKeyVecs * 64];
+  __shared__ __align__(16) f16x8 value_tile[kBuffers][2 * kTiles * 64];
+  __shared__ int nan_tile[2][4];  // whether a wave took NaN codes out of the values it wrote
+
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int split = blockIdx.y;
+  Place p;
+  if (!attend_place(a, 64 * MT, lane, p)) return;
+  const int tile0 = p.tile * 64 * MT, row0 = tile0 + wave * 16 * MT, h = p.h;
+  const int lim_first = seen_by(a, p, tile0), lim_lo = seen_by(a, p, row0), lim_wave = row0 < p.rows ? seen_by(a, p, row0 + 16 * MT - 1) : 0;
+  const int lim_hi = seen_by(a, p, tile0 + 64 * MT - 1);
+  const int tiles = lim_hi > 0 ? (lim_hi + 63) >> 6 : 0;
+  const int t_begin = split * a.split_tiles;
+  const int t_end = split == a.splits - 1 ? tiles : min(tiles, t_begin + a.split_tiles);
+  if (split > 0 && t_begin >= tiles) return;
+
+  vec qf[MT][kSteps];
+  int lim[MT];
+  load_queries<D, BF, MT>(a, p, row0, m, g, qf, lim);
+  f32x4 acc[kTiles][MT];
+  float M[MT], l[MT];
+#pragma unroll
+  for (int r = 0; r < MT; ++r) {
+    M[r] = -INFINITY;
+    l[r] = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  const PageWalk walk(a, p);
+  u32x4 stage[kEach];
+  u32x2 stage_half;
+  // the wave's groups of tile t, from its lanes' pages (all keys or all values, but for a D with an odd share)
+  constexpr bool kMixed = kKeys % kEach != 0;
+  const bool keys = wave * kEach < kKeys;
+  const int64_t lane_k = (m & 3) * 16 + g * 256, lane_v = m * 16;
+  const auto load = [&](int pk, int pv, int t) {
+    const uint8_t* ka = walk.unit(a.k, pk, 4 * t + (m >> 2), 16 * D) + lane_k;
+    const uint8_t* va = walk.unit(a.v, pv, 4 * t + g, 16 * D) + lane_v;
+    const uint8_t* at = keys ? ka : va;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int q = wave * kEach + j;
+      if (kGroups % 4 != 0 && q >= kGroups) break;
+      if (kMixed) at = q < kKeys ? ka : va;
+      const int off = q < kKeys ? (q / kWhole) * 64 + (q % kWhole) * 1024 : (q - kKeys) * 256;
+      stage[j] = *reinterpret_cast<const u32x4*>(at + off);
+    }
+    if (kHalf)
+      stage_half = *reinterpret_cast<const u32x2*>(ka - g * 256 + wave * 64 + (4 * kWhole + (g >> 1)) * 256 + (g & 1) * 8);
+  };
+  const auto put = [&](int t, bool ok) {
+    const int b = t & (kBuffers - 1);
+    if (64 * (t + 1) > p.len || __ballot(ok) != ~0ull) {  // values past the sequence's end are not the cache's: any bytes
+      const int keep = ok ? max(p.len - (64 * t + 16 * g), 0) : 0;
+#pragma unroll
+      for (int j = 0; j < kEach; ++j)
+        if (wave * kEach + j >= kKeys) stage[j] = low_bytes(stage[j], keep);
+    }
+    if (64 * (t + 1) > lim_first) {  // some rows do not see all of the tile
+      uint32_t any = 0;
+#pragma unroll
+      for (int j = 0; j < kEach; ++j)
+        if (wave * kEach + j >= kKeys && wave * kEach + j < kGroups) any |= nan_any(stage[j]);
+      const bool bad = __ballot(any != 0) != 0;
+      if (bad) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+          if (wave * kEach + j >= kKeys) stage[j] = nan_out(stage[j]);
+      }
+      if (lane == 0) nan_tile[t & 1][wave] = bad;
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const int q = wave * kEach + j;
+      if (kGroups % 4 != 0 && q >= kGroups) break;
+      if (kMixed ? q < kKeys : keys) {
+        vec* to = key_tile[b] + (q / kWhole * kSteps + 2 * (q % kWhole)) * 64 + lane;
+        to[0] = E::widen(stage[j][0], stage[j][1]);
+        to[64] = E::widen(stage[j][2], stage[j][3]);
+      } else {
+        f16x8* to = value_tile[b] + 2 * (q - kKeys) * 64 + lane;
+        to[0] = Elem<false>::widen(stage[j][0], stage[j][1]);
+        to[64] = Elem<false>::widen(stage[j][2], stage[j][3]);
+      }
+    }
+    if (kHalf) key_tile[b][(wave * kSteps + kSteps - 1) * 64 + lane] = E::widen(stage_half[0], stage_half[1]);
+  };
+
+  if (t_begin < t_end) {
+    bool ok, ok_k;
+    int pk = walk.valid(walk.page(4 * t_begin + (m >> 2)), ok_k), pv = walk.valid(walk.page(4 * t_begin + g), ok);
+    load(pk, pv, t_begin);
+    int ke = a.k_exp[(int64_t)pv * a.heads + h], ve = a.v_exp[(int64_t)pv * a.heads + h];
+    int pk_next = walk.page(4 * (t_begin + 1) + (m >> 2)), pv_next = walk.page(4 * (t_begin + 1) + g);
+    put(t_begin, ok);
+    __syncthreads();
+    for (int t = t_begin; t < t_end; ++t) {
+      const float c_g = a.scale_log2 * pow2i(ke), ve_g = (float)ve, inv_v = pow2i(-ve);
+      const bool ok_now = ok;
+      const bool more = t + 1 < t_end;
+      if (more) {
+        pk = walk.valid(pk_next, ok_k);
+        pv = walk.valid(pv_next, ok);
+        load(pk, pv, t + 1);
+        ke = a.k_exp[(int64_t)pv * a.heads + h];
+        ve = a.v_exp[(int64_t)pv * a.heads + h];
+        pk_next = walk.page(4 * (t + 2) + (m >> 2));
+        pv_next = walk.page(4 * (t + 2) + g);
+      }
+      if (64 * t < lim_wave) {
+        const vec* kt = key_tile[t & (kBuffers - 1)] + lane;
+        const f16x8* vt = value_tile[t & (kBuffers - 1)] + lane;
+        f32x4 sc[4][MT];
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) {
+#pragma unroll
+          for (int r = 0; r < MT; ++r) sc[tt][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int st = 0; st < kSteps; ++st) {
+            const vec kf = kt[(tt * kSteps + st) * 64];
+#pragma unroll
+            for (int r = 0; r < MT; ++r) sc[tt][r] = E::mfma(kf, qf[r][st], sc[tt][r]);
+          }
+        }
+        const bool masked = 64 * (t + 1) > lim_lo || __ballot(ok_now) != ~0ull;
+        const int first = 64 * t + 16 * g;
+        int upto[MT];
+#pragma unroll
+        for (int r = 0; r < MT; ++r) upto[r] = ok_now ? lim[r] - first : 0;
+        f16x8 pf[MT][2];
+        float alpha[MT];
+        const bool grown = masked ? weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, alpha, pf)
+                                  : weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, alpha, pf);
+        if (grown) {
+#pragma unroll
+          for (int r = 0; r < MT; ++r)
+#pragma unroll
+            for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] *= alpha[r];
+        }
+        if (64 * (t + 1) > lim_first && (nan_tile[t & 1][0] | nan_tile[t & 1][1] | nan_tile[t & 1][2] | nan_tile[t & 1][3])) {
+          // (rare: the tile was written without its NaN codes, which are read from the cache again)
+          const uint8_t* va = walk.unit(a.v, walk.valid(walk.page(4 * t + g), ok_k), 4 * t + g, 16 * D) + lane_v;
+          const int keep = ok_now ? max(p.len - first, 0) : 0;
+#pragma unroll
+          for (int dt = 0; dt < kTiles; ++dt)
+            mark_nan<MT>(low_bytes(*reinterpret_cast<const u32x4*>(va + dt * 256), keep), upto, acc[dt]);
+        }
+#pragma unroll
+        for (int dt = 0; dt < kTiles; ++dt) {
+          const f16x8 v[2] = {vt[2 * dt * 64], vt[(2 * dt + 1) * 64]};
+          add_values<MT>(v, pf, acc[dt]);
+        }
+      }
+      if (kBuffers == 1) __syncthreads();  // every wave is done with the tile
+      if (more) {
+        put(t + 1, ok);
+        __syncthreads();
+      }
+    }
+  }
+
+  const int64_t heads_q = (int64_t)a.heads * a.group;
+#pragma unroll
+  for (int r = 0; r < MT; ++r) {
+    const float ls = row_sum4(l[r]);
+    const int row = row0 + 16 * r + m;
+    if (row >= p.rows) continue;
+    const int i = row / a.group;
+    const int64_t id = (p.start + i) * heads_q + h * a.group + (row - i * a.group);
+    if (a.splits == 1) {
+      const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
+      one* o = static_cast<one*>(a.out) + id * D + 4 * g;
+#pragma unroll
+      for (int dt = 0; dt < kTiles; ++dt) {
+        typedef one one4 __attribute__((ext_vector_type(4)));
+        one4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (one)(ls == 0.0f ? 0.0f : acc[dt][r][e] * inv);
+        *reinterpret_cast<one4*>(o + 16 * dt) = w;
+      }
+      if (a.lse && g == 0) a.lse[id] = ls == 0.0f ? -INFINITY : (M[r] + log2f(ls)) * 0.693147180559945f;
+    } else {
+      float* o = a.part + (id * a.splits + split) * D + 4 * g;
+#pragma unroll
+      for (int dt = 0; dt < kTiles; ++dt) *reinterpret_cast<f32x4*>(o + 16 * dt) = acc[dt][r];
+      if (g == 0) {
+        a.part_ml[2 * (id * a.splits + split)] = M[r];
+        a.part_ml[2 * (id * a.splits + split) + 1] = ls;
       }
     }
   }
@@ -536,8 +769,8 @@ AttendPlan attend_plan(const CacheView& c, int64_t T, int64_t S, int64_t width, 
   if (max_length > 0 && max_length < tokens) tokens = max_length;
   const int64_t tiles = (tokens + 63) >> 6;
   const int64_t base = p.slots * c.heads;
-  // enough workgroups for four on each CU, each with at least 8 tiles (2 a wave)
-  int64_t splits = (1024 + base - 1) / base;
+  // enough workgroups for four on each CU (two where the rows are many), each with at least 8 tiles (2 a wave)
+  int64_t splits = p.wide ? 512 / base : (1024 + base - 1) / base;
   if (splits > (tiles + 7) / 8) splits = (tiles + 7) / 8;
   if (splits > 128) splits = 128;
   if (splits < 1) splits = 1;
@@ -548,21 +781,25 @@ AttendPlan attend_plan(const CacheView& c, int64_t T, int64_t S, int64_t width, 
   return p;
 }
 
-template <int D, bool BF, int MT, bool WIDE>
-void attend_one(const AttendArgs& a, int64_t slots, hipStream_t st) {
-  attend_kernel<D, BF, MT, WIDE><<<dim3((unsigned)(slots * a.heads), (unsigned)a.splits), 256, 0, st>>>(a);
+template <int D, bool BF, int MT>
+void attend_few(const AttendArgs& a, int64_t slots, hipStream_t st) {
+  attend_kernel<D, BF, MT><<<dim3((unsigned)(slots * a.heads), (unsigned)a.splits), 256, 0, st>>>(a);
+}
+template <int D, bool BF, int MT>
+void attend_many(const AttendArgs& a, int64_t slots, hipStream_t st) {
+  attend_wide_kernel<D, BF, MT><<<dim3((unsigned)(slots * a.heads), (unsigned)a.splits), 256, 0, st>>>(a);
 }
 
 template <int D, bool BF>
 hipError_t attend_launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
   if (p.wide) {
-    attend_one<D, BF, D == 256 ? 1 : 2, true>(a, p.slots, st);
+    attend_many<D, BF, D == 256 ? 1 : 2>(a, p.slots, st);
   } else if (p.mt == 1) {
-    attend_one<D, BF, 1, false>(a, p.slots, st);
+    attend_few<D, BF, 1>(a, p.slots, st);
   } else if (p.mt == 2) {
-    attend_one<D, BF, 2, false>(a, p.slots, st);
+    attend_few<D, BF, 2>(a, p.slots, st);
   } else if constexpr (D <= 128) {
-    attend_one<D, BF, 4, false>(a, p.slots, st);
+    attend_few<D, BF, 4>(a, p.slots, st);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
@@ -609,7 +846,8 @@ hipError_t launch_cache_attention(const CacheView& c, int layer, const void* q, 
   a.per_seq = p.per_seq;
   a.splits = p.splits;
   a.split_tiles = p.split_tiles;
-  a.scale_log2 = scale * 1.4426950408889634f;
+  a.scale_log2 = fabsf(scale) * 1.4426950408889634f;
+  a.negative = scale < 0.0f;
   const bool bf = dtype == MDSS_BF16;
   switch (c.d) {
     case 64: return bf ? attend_launch<64, true>(a, p, st) : attend_launch<64, false>(a, p, st);
