@@ -85,20 +85,4 @@ __device__ __forceinline__ int64_t slot_first(const int32_t* starts, int s, int 
   return (int64_t)starts[s] * num / den + (int64_t)extra * s;
 }
 
-// Copies 16 KB pieces of pages: piece i of `pieces` of copy c, by the whole workgroup of 256 threads.
-constexpr int kPiece = 16384;
-__device__ __forceinline__ void copy_piece(const uint8_t* __restrict__ src, uint8_t* __restrict__ dst, int bytes) {
-  u32x4 r[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int at = ((int)threadIdx.x + 256 * j) * 16;
-    if (at < bytes) r[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + at));
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int at = ((int)threadIdx.x + 256 * j) * 16;
-    if (at < bytes) __builtin_nontemporal_store(r[j], reinterpret_cast<u32x4*>(dst + at));
-  }
-}
-
 }  // namespace mdss
