@@ -1,6 +1,7 @@
 """Beam search's step: the best continuations over beams and vocabulary, and the reordering of states by parent."""
 from __future__ import annotations
 
+import math
 from typing import Optional
 
 import torch
@@ -37,10 +38,10 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, done: Optional[torch
     if row_status is not None:
         _need(row_status, "row_status", torch.int32, (B * W,), dev)
     n = W if n is None else n
-    parent = torch.empty((B, n), dtype=torch.int32, device=dev)
-    token = torch.empty((B, n), dtype=torch.int32, device=dev)
-    score = torch.empty((B, n), dtype=torch.float32, device=dev)
-    done_out = torch.empty((B, n), dtype=torch.uint8, device=dev)
+    parent = torch.empty_strided((B, n), (n, 1), dtype=torch.int32, device=dev)
+    token = torch.empty_like(parent)
+    score = torch.empty_strided((B, n), (n, 1), dtype=torch.float32, device=dev)
+    done_out = torch.empty_strided((B, n), (n, 1), dtype=torch.uint8, device=dev)
     workspace = _scratch(dev, lib.mdss_workspace_bytes_beam(B, W, V, n), workspace)
     _check("mdss_beam_select",
            lib.mdss_beam_select(_ptr(logits), _DTYPES[logits.dtype], stride, _ptr(scores), _ptr(done), B, W, V, n, eos,
@@ -52,22 +53,20 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, done: Optional[torch
 def beam_reorder(state: torch.Tensor, parent: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """``out[b][j] = state[b][parent[b][j]]`` for a state ``[B][W][...]`` of any type; zeros where the parent is -1."""
     lib = load_library()
-    if state.dim() < 2 or parent.dim() != 2:
+    shape = state.shape
+    if len(shape) < 2 or parent.dim() != 2:
         raise ValueError("state must be [B][W][...] and parent [B][n]")
-    if state.device.type != "cuda":
+    if not state.is_cuda:
         raise ValueError("state must be a GPU tensor")
-    B, W = state.shape[:2]
-    n = parent.shape[1]
-    _need(state, "state", state.dtype, tuple(state.shape), state.device)
+    if not state.is_contiguous():
+        raise ValueError("state must be contiguous")
+    B, W, n = shape[0], shape[1], parent.shape[1]
     _need(parent, "parent", torch.int32, (B, n), state.device)
-    shape = (B, n) + tuple(state.shape[2:])
     if out is None:
-        out = torch.empty(shape, dtype=state.dtype, device=state.device)
+        out = torch.empty_like(state) if n == W else torch.empty((B, n) + shape[2:], dtype=state.dtype, device=state.device)
     else:
-        _need(out, "out", state.dtype, shape, state.device)
-    row = state.element_size()
-    for x in state.shape[2:]:
-        row *= x
+        _need(out, "out", state.dtype, (B, n) + shape[2:], state.device)
+    row = state.element_size() * math.prod(shape[2:])
     _check("mdss_beam_reorder",
            lib.mdss_beam_reorder(_ptr(state), _ptr(parent), B, W, n, row, _ptr(out), _stream(state.device)))
     return out

@@ -13,8 +13,8 @@ many for each), the last of its ``lengths[s]`` tokens.
 """
 from __future__ import annotations
 
-import ctypes
 import math
+import struct
 from typing import Optional
 
 import torch
@@ -24,10 +24,8 @@ from .binding import _check, _need, _ptr, _stream, _workspace, load_library
 _DTYPES = {torch.bfloat16: 1, torch.float16: 2}
 
 
-class _Desc(ctypes.Structure):
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p),
-                ("v_exp", ctypes.c_void_p), ("pages", ctypes.c_int64), ("layers", ctypes.c_int32),
-                ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+# mdss_cache of the C ABI: k, v, k_exp, v_exp, pages, layers, heads, head_dim, page_size
+_DESC = struct.Struct("PPPPqiiii")
 
 
 class PagedCache:
@@ -38,25 +36,25 @@ class PagedCache:
     k_exp, v_exp [layers][pages][heads]                                   int8; a value is code * 2**exp
     """
 
-    __slots__ = ("k", "v", "k_exp", "v_exp", "layers", "pages", "heads", "head_dim", "page_size", "device", "_desc",
-                 "_ref")
+    __slots__ = ("k", "v", "k_exp", "v_exp", "layers", "pages", "heads", "head_dim", "page_size", "device", "_ref")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor):
-        if k.dim() != 7 or k.shape[5] != 16 or k.shape[6] != 16:
+        shape = k.shape
+        if len(shape) != 7 or shape[5] != 16 or shape[6] != 16:
             raise ValueError("k must be [layers][pages][heads][page_size / 16][head_dim / 16][16][16]")
-        if k.device.type != "cuda":
+        if not k.is_cuda:
             raise ValueError("k must be a GPU tensor")
-        layers, pages, heads, units, chunks = k.shape[:5]
-        _need(k, "k", torch.uint8, tuple(k.shape), k.device)
-        _need(v, "v", torch.uint8, (layers, pages, heads, units, 16 * chunks, 16), k.device)
-        _need(k_exp, "k_exp", torch.int8, (layers, pages, heads), k.device)
-        _need(v_exp, "v_exp", torch.int8, (layers, pages, heads), k.device)
+        layers, pages, heads, units, chunks = shape[:5]
+        device = k.device
+        _need(k, "k", torch.uint8, shape, device)
+        _need(v, "v", torch.uint8, (layers, pages, heads, units, 16 * chunks, 16), device)
+        _need(k_exp, "k_exp", torch.int8, (layers, pages, heads), device)
+        _need(v_exp, "v_exp", torch.int8, (layers, pages, heads), device)
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
-        self.layers, self.pages, self.heads = layers, pages, heads
-        self.head_dim, self.page_size, self.device = 16 * chunks, 16 * units, k.device
-        self._desc = _Desc(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), pages, layers, heads,
-                           16 * chunks, 16 * units)
-        self._ref = ctypes.byref(self._desc)
+        self.layers, self.pages, self.heads, self.device = layers, pages, heads, device
+        self.head_dim, self.page_size = 16 * chunks, 16 * units
+        self._ref = _DESC.pack(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), pages, layers, heads,
+                               16 * chunks, 16 * units)
 
     @classmethod
     def empty(cls, layers: int, pages: int, heads: int, head_dim: int, page_size: int = 64,
@@ -139,7 +137,7 @@ def cache_attention(q: torch.Tensor, cache: PagedCache, layer: int, starts: Opti
     T, heads_q = q.shape[0], q.shape[1]
     dev = cache.device
     if out is None:
-        out = torch.empty((T, heads_q, cache.head_dim), dtype=q.dtype, device=dev)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     else:
         _need(out, "out", q.dtype, (T, heads_q, cache.head_dim), dev)
     lse = torch.empty((T, heads_q), dtype=torch.float32, device=dev) if want_lse else None
@@ -173,8 +171,8 @@ def cache_fork(cache: PagedCache, table: torch.Tensor, lengths: torch.Tensor, re
         if x is not None:
             _need(x, name, torch.int32, (S_out,), dev)
     _status(row_status, S_out, dev)
-    table_out = torch.empty((S_out, width), dtype=torch.int32, device=dev)
-    lengths_out = torch.empty(S_out, dtype=torch.int32, device=dev)
+    table_out = torch.empty_strided((S_out, width), (width, 1), dtype=torch.int32, device=dev)
+    lengths_out = torch.empty_strided((S_out,), (1,), dtype=torch.int32, device=dev)
     refs_out = torch.empty_like(refs)
     workspace = _scratch(dev, lib.mdss_workspace_bytes_cache_fork(cache._ref, S_out), workspace)
     _check("mdss_cache_fork",
@@ -192,7 +190,7 @@ def cache_compact(cache: PagedCache, table: torch.Tensor, lengths: torch.Tensor,
     dev = cache.device
     _need(refs, "refs", torch.int32, (cache.pages,), dev)
     table_out, refs_out = torch.empty_like(table), torch.empty_like(refs)
-    used = torch.empty((), dtype=torch.int32, device=dev)
+    used = torch.empty_strided((), (), dtype=torch.int32, device=dev)
     workspace = _scratch(dev, lib.mdss_workspace_bytes_cache_compact(cache._ref), workspace)
     _check("mdss_cache_compact",
            lib.mdss_cache_compact(cache._ref, _ptr(table), _ptr(lengths), S, width, _ptr(refs), _ptr(table_out),

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2410_18234_amd as mdss
-from paper_2410_18234_amd.cache import _Desc
+from paper_2410_18234_amd.cache import _DESC
 
 FAKE = ctypes.c_void_p(0x1000)  # never dereferenced: every call below fails validation first
 ODD = ctypes.c_void_p(0x1001)
@@ -19,7 +19,7 @@ def lib():
 
 
 def desc(k=0x1000, v=0x1000, pages=8, layers=2, heads=2, d=64, ps=16):
-    return ctypes.byref(_Desc(k, v, 0x1000, 0x1000, pages, layers, heads, d, ps))
+    return _DESC.pack(k, v, 0x1000, 0x1000, pages, layers, heads, d, ps)
 
 
 BAD_SHAPES = [(dict(pages=0), ESHAPE), (dict(pages=(1 << 24) + 1), ESHAPE), (dict(layers=0), ESHAPE), (dict(heads=0), ESHAPE),
