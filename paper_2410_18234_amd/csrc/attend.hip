@@ -302,8 +302,10 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
   constexpr bool kHalf = D % 64 != 0;  // and one of 8 bytes
   constexpr int kTiles = D / 16;       // accumulator tiles over d
   constexpr int kPad = D + 4;
-  __shared__ __align__(16) float joined[4 * 16 * kPad];
-  __shared__ float joined_ml[4 * 16 * 2];
+  constexpr int NW = 4;  // waves
+  __shared__ __align__(16) float joined[NW * 16 * kPad];
+  __shared__ float joined_ml[NW * 16 * 2];
+  __shared__ __align__(16) vec queries[MT * kSteps * 64];  // the same for all four waves: LDS spares their registers
 
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -318,9 +320,18 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
   // a split without tokens for any of the rows has nothing to say (the first one always speaks)
   if (split > 0 && t_begin >= tiles) return;
 
-  vec qf[MT][kSteps];
   int lim[MT];
-  load_queries<D, BF, MT>(a, p, row0, m, g, qf, lim);
+  {
+    vec qf[MT][kSteps];
+    load_queries<D, BF, MT>(a, p, row0, m, g, qf, lim);
+    if (wave == 0) {
+#pragma unroll
+      for (int r = 0; r < MT; ++r)
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) queries[(r * kSteps + st) * 64 + lane] = qf[r][st];
+    }
+    __syncthreads();
+  }
   f32x4 acc[kTiles][MT];
   float M[MT], l[MT];
 #pragma unroll
@@ -350,8 +361,8 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
     int pk = walk.valid(walk.page(4 * t0 + (m >> 2)), ok_k), pv = walk.valid(walk.page(4 * t0 + g), ok);
     load_k(pk, t0);
     int ke = a.k_exp[(int64_t)pv * a.heads + h], ve = a.v_exp[(int64_t)pv * a.heads + h];
-    int pk_next = walk.page(4 * (t0 + 4) + (m >> 2)), pv_next = walk.page(4 * (t0 + 4) + g);
-    for (int t = t0; t < t_end; t += 4) {
+    int pk_next = walk.page(4 * (t0 + NW) + (m >> 2)), pv_next = walk.page(4 * (t0 + NW) + g);
+    for (int t = t0; t < t_end; t += NW) {
       u32x4 vc[kTiles];
       {
         const uint8_t* at = walk.unit(a.v, pv, 4 * t + g, 16 * D) + m * 16;
@@ -360,27 +371,30 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
       }
       f32x4 sc[4][MT];
 #pragma unroll
-      for (int tt = 0; tt < 4; ++tt) {
+      for (int st = 0; st < kSteps; ++st) {
+        vec qf[MT];
 #pragma unroll
-        for (int r = 0; r < MT; ++r) sc[tt][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int r = 0; r < MT; ++r) qf[r] = queries[(r * kSteps + st) * 64 + lane];
 #pragma unroll
-        for (int st = 0; st < kSteps; ++st) {
+        for (int tt = 0; tt < 4; ++tt) {
           const vec kf = (kHalf && st == kSteps - 1) ? E::widen(kh[tt][0], kh[tt][1])
                                                       : E::widen(kc[tt][st >> 1][2 * (st & 1)], kc[tt][st >> 1][2 * (st & 1) + 1]);
 #pragma unroll
-          for (int r = 0; r < MT; ++r) sc[tt][r] = E::mfma(kf, qf[r][st], sc[tt][r]);
+          for (int r = 0; r < MT; ++r)
+            sc[tt][r] = E::mfma(kf, qf[r], st == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sc[tt][r]);
         }
       }
       const float c_g = a.scale_log2 * pow2i(ke), ve_g = (float)ve, inv_v = pow2i(-ve);
       const bool ok_now = ok;
       // the next tile's keys, exponents, and the page ids after it
+      __builtin_amdgcn_sched_barrier(0);  // (into the registers of this one's)
       pk = walk.valid(pk_next, ok_k);
-      load_k(pk, t + 4);
+      load_k(pk, t + NW);
       pv = walk.valid(pv_next, ok);
       ke = a.k_exp[(int64_t)pv * a.heads + h];
       ve = a.v_exp[(int64_t)pv * a.heads + h];
-      pk_next = walk.page(4 * (t + 8) + (m >> 2));
-      pv_next = walk.page(4 * (t + 8) + g);
+      pk_next = walk.page(4 * (t + 2 * NW) + (m >> 2));
+      pv_next = walk.page(4 * (t + 2 * NW) + g);
 
       const bool masked = 64 * (t + 1) > lim_lo || __ballot(ok_now) != ~0ull;
       const int first = 64 * t + 16 * g;  // the lane's first token
@@ -397,36 +411,37 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
 #pragma unroll
           for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] *= alpha[r];
       }
+      // what lies past the sequence's end is not the cache's: any bytes
+      const int keep = ok_now ? min(max(p.len - first, 0), 16) : 0;
+      bool bad = false;
       if (masked) {
-        // what lies past the sequence's end is not the cache's: any bytes
-        const int keep = ok_now ? min(max(p.len - first, 0), 16) : 0;
         uint32_t any = 0;
 #pragma unroll
-        for (int dt = 0; dt < kTiles; ++dt) {
-          vc[dt] = low_bytes(vc[dt], keep);
-          any |= nan_any(vc[dt]);
-        }
-        if (__ballot(any != 0) != 0) {
-#pragma unroll
-          for (int dt = 0; dt < kTiles; ++dt) {
-            mark_nan<MT>(vc[dt], upto, acc[dt]);
-            vc[dt] = nan_out(vc[dt]);
-          }
-        }
+        for (int dt = 0; dt < kTiles; ++dt) any |= nan_any(vc[dt]);
+        bad = __ballot(any != 0) != 0;
       }
 #pragma unroll
       for (int dt = 0; dt < kTiles; ++dt) {
-        const f16x8 v[2] = {Elem<false>::widen(vc[dt][0], vc[dt][1]), Elem<false>::widen(vc[dt][2], vc[dt][3])};
+        u32x4 c = vc[dt];
+        if (masked) {
+          c = low_bytes(c, keep);
+          if (bad) {
+            mark_nan<MT>(c, upto, acc[dt]);
+            c = nan_out(c);
+          }
+        }
+        const f16x8 v[2] = {Elem<false>::widen(c[0], c[1]), Elem<false>::widen(c[2], c[3])};
         add_values<MT>(v, pf, acc[dt]);
       }
     }
   }
 
-  // join the four waves, 16 rows at a time: thread -> a row and D / 16 of its elements
+  // join the four waves, 16 rows at a time: thread -> a row and a share of its elements
 #pragma unroll
   for (int r = 0; r < MT; ++r) l[r] = row_sum4(l[r]);
   const int64_t heads_q = (int64_t)a.heads * a.group;
-  const int jr = threadIdx.x >> 4, jd = (threadIdx.x & 15) * (D / 16);
+  constexpr int kShare = D / (4 * NW);  // elements of a thread
+  const int jr = threadIdx.x / (4 * NW), jd = threadIdx.x % (4 * NW) * kShare;
 #pragma unroll
   for (int r = 0; r < MT; ++r) {
     if (r > 0) __syncthreads();
@@ -438,11 +453,11 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
       joined_ml[(wave * 16 + m) * 2 + 1] = l[r];
     }
     __syncthreads();
-    float top = -INFINITY, lsum = 0.0f, wgt[4];
+    float top = -INFINITY, lsum = 0.0f, wgt[NW];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = fmaxf(top, joined_ml[(i * 16 + jr) * 2]);
+    for (int i = 0; i < NW; ++i) top = fmaxf(top, joined_ml[(i * 16 + jr) * 2]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NW; ++i) {
       wgt[i] = frame_weight(joined_ml[(i * 16 + jr) * 2], top);
       lsum = fmaf(wgt[i], joined_ml[(i * 16 + jr) * 2 + 1], lsum);
     }
@@ -452,10 +467,10 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
       const int64_t id = (p.start + i) * heads_q + h * a.group + (row - i * a.group);  // row of [T][heads_q]
       const float inv = lsum == 0.0f ? 0.0f : 1.0f / lsum;
 #pragma unroll
-      for (int e = 0; e < D / 16; e += 2) {
+      for (int e = 0; e < kShare; e += 2) {
         f32x2 o = {0.0f, 0.0f};
 #pragma unroll
-        for (int w4 = 0; w4 < 4; ++w4) {
+        for (int w4 = 0; w4 < NW; ++w4) {
           const f32x2 x = *reinterpret_cast<const f32x2*>(joined + (w4 * 16 + jr) * kPad + jd + e);
           o[0] = fmaf(wgt[w4], x[0], o[0]);
           o[1] = fmaf(wgt[w4], x[1], o[1]);
@@ -468,7 +483,7 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
           *reinterpret_cast<f32x2*>(a.part + (id * a.splits + split) * D + jd + e) = o;
         }
       }
-      if ((threadIdx.x & 15) == 0) {
+      if (jd == 0) {
         if (a.splits == 1) {
           if (a.lse) a.lse[id] = lsum == 0.0f ? -INFINITY : (top + log2f(lsum)) * 0.693147180559945f;
         } else {
@@ -768,9 +783,14 @@ AttendPlan attend_plan(const CacheView& c, int64_t T, int64_t S, int64_t width, 
   int64_t tokens = width << c.page_shift;
   if (max_length > 0 && max_length < tokens) tokens = max_length;
   const int64_t tiles = (tokens + 63) >> 6;
-  const int64_t base = p.slots * c.heads;
-  // enough workgroups for four on each CU (two where the rows are many), each with at least 8 tiles (2 a wave)
-  int64_t splits = p.wide ? 512 / base : (1024 + base - 1) / base;
+  // (ragged slots are an upper bound: rows that hardly fill their tiles take one a sequence)
+  const int64_t full = (T * group + tile_rows - 1) / tile_rows, base = (p.per_seq ? p.slots : full > S ? full : S) * c.heads;
+  // Few rows: as many workgroups as the 256 CUs hold at a time by the kernels' registers (4 x 131072 tokens: 768 workgroups
+  // 190 us, 512 209, 1024 200), each with at least 8 tiles; none of it below 2048 tokens, where the second launch costs
+  // more than the tiles' latency (one sequence: 1024 tokens 12.8 us whole, 16.3 split; 4096 23.7 and 16.7).
+  // Many rows: two workgroups a CU, and only where that leaves half of them idle.
+  const int resident = c.d * p.mt <= 64 ? 4 : c.d * p.mt <= 128 ? 3 : c.d <= 128 && p.mt == 2 ? 2 : 1;
+  int64_t splits = p.wide ? 512 / base : tiles < 32 ? 1 : (256 * resident + base / 2) / base;
   if (splits > (tiles + 7) / 8) splits = (tiles + 7) / 8;
   if (splits > 128) splits = 128;
   if (splits < 1) splits = 1;
