@@ -156,7 +156,7 @@ __device__ __forceinline__ bool attend_place(const AttendArgs& a, int tile_rows,
   }
   if (p.start < 0 || p.n <= 0 || p.start + p.n > a.T) return false;  // no rows, or starts that do not ascend within T
   p.rows = p.n * a.group;
-  if (p.tile * tile_rows >= p.rows) return false;
+  if (p.tile < 0 || p.tile >= (p.rows + tile_rows - 1) / tile_rows) return false;  // (below 0: starts[0] is not 0)
   const int length = a.lengths[p.s];
   p.len = max(0, min(length, (int)min(a.width << a.page_shift, (int64_t)INT32_MAX)));
   p.before = length - p.n;
