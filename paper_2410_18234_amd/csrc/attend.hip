@@ -785,12 +785,28 @@ AttendPlan attend_plan(const CacheView& c, int64_t T, int64_t S, int64_t width, 
   const int64_t tiles = (tokens + 63) >> 6;
   // (ragged slots are an upper bound: rows that hardly fill their tiles take one a sequence)
   const int64_t full = (T * group + tile_rows - 1) / tile_rows, base = (p.per_seq ? p.slots : full > S ? full : S) * c.heads;
-  // Few rows: as many workgroups as the 256 CUs hold at a time by the kernels' registers (4 x 131072 tokens: 768 workgroups
-  // 190 us, 512 209, 1024 200), each with at least 8 tiles; none of it below 2048 tokens, where the second launch costs
-  // more than the tiles' latency (one sequence: 1024 tokens 12.8 us whole, 16.3 split; 4096 23.7 and 16.7).
+  // Few rows: each split has at least 8 tiles; none below 2048 tokens, where the second launch costs more than the tiles'
+  // latency (one sequence: 1024 tokens 12.8 us whole, 16.3 split; 4096 23.7 and 16.7).  As many workgroups as the 256 CUs
+  // hold at a time by the kernels' registers, but where that is three of one row tile:
+  //   up to 32 (sequence, head) pairs take two a CU (4 x 131072 tokens, 8 heads: 512 workgroups 194 us, 768 214, 1536 215), and
+  //   few of them fewer splits, which are joined one after the other (1 x 100000: 32 splits 47 us, 64 51, 96 54);
+  //   more pairs take six a CU, so that unlike lengths even out (16 x up to 30000, a quarter up: 1536 workgroups 77 us, 768 98,
+  //   512 96; all of 30000: 193, 197, 177; 32 x up to 8192: 46, 55, 58).
   // Many rows: two workgroups a CU, and only where that leaves half of them idle.
   const int resident = c.d * p.mt <= 64 ? 4 : c.d * p.mt <= 128 ? 3 : c.d <= 128 && p.mt == 2 ? 2 : 1;
-  int64_t splits = p.wide ? 512 / base : tiles < 32 ? 1 : (256 * resident + base / 2) / base;
+  int64_t splits;
+  if (p.wide) {
+    splits = 512 / base;
+  } else if (tiles < 32) {
+    splits = 1;
+  } else if (p.mt > 1 || resident != 3) {
+    splits = (256 * resident + base / 2) / base;
+  } else if (base > 32) {
+    splits = 1536 / base;
+  } else {
+    const int64_t most = base > 8 ? 32 : 256 / base;
+    splits = 512 / base < most ? 512 / base : most;
+  }
   if (splits > (tiles + 7) / 8) splits = (tiles + 7) / 8;
   if (splits > 128) splits = 128;
   if (splits < 1) splits = 1;
