@@ -136,7 +136,8 @@ struct Place {
   int len, before;  // cached tokens (as far as the table goes); those before the new ones (negative: the first rows see nothing)
 };
 // The head is the fastest index of the grid: the row tiles that read one head's pages run on the same XCD where heads
-// are a multiple of 8 (workgroups go round the XCDs in order), and find them in its L2.
+// are a multiple of 8 (workgroups go round the XCDs in order), and find them in its L2.  A sequence's last rows, which see the
+// most tokens, start first (a prompt of 3000 tokens, 64 query heads: 205 us, 246 the other way round).
 __device__ __forceinline__ bool attend_place(const AttendArgs& a, int tile_rows, int lane, Place& p) {
   const int slot = blockIdx.x / a.heads;
   p.h = blockIdx.x - slot * a.heads;
@@ -156,7 +157,9 @@ __device__ __forceinline__ bool attend_place(const AttendArgs& a, int tile_rows,
   }
   if (p.start < 0 || p.n <= 0 || p.start + p.n > a.T) return false;  // no rows, or starts that do not ascend within T
   p.rows = p.n * a.group;
-  if (p.tile < 0 || p.tile >= (p.rows + tile_rows - 1) / tile_rows) return false;  // (below 0: starts[0] is not 0)
+  const int tiles = (p.rows + tile_rows - 1) / tile_rows;
+  if (p.tile < 0 || p.tile >= tiles) return false;  // (below 0: starts[0] is not 0)
+  p.tile = tiles - 1 - p.tile;
   const int length = a.lengths[p.s];
   p.len = max(0, min(length, (int)min(a.width << a.page_shift, (int64_t)INT32_MAX)));
   p.before = length - p.n;
