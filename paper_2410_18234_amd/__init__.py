@@ -5,6 +5,9 @@ Thin Python binding over the C ABI of ``libmdss.so`` (declared in
 the HIP kernels of the library.  PyTorch supplies device buffers and the
 current HIP stream.
 
+Beside it, a paged 8-bit cache of keys and values (``PagedCache`` and the ``cache_*`` calls) and beam search's step
+(``beam_select``, ``beam_reorder``).
+
 Notation: ``p`` = target distribution, ``q`` = draft distribution (the paper
 writes them the other way round), both ``[B][V]`` fp32 on the GPU.
 """
