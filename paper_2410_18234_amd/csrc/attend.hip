@@ -296,9 +296,10 @@ __device__ __forceinline__ void add_values(const f16x8 (&v)[2], const f16x8 (&pf
 // Few rows: the four waves of a workgroup take the same rows against tiles of 64 tokens in turn, straight from memory
 // to registers, and join at the end.  Bound by memory: a tile's keys are loaded while the one before is
 // weighed, its values while its keys are multiplied.  4 x 131072 tokens, 8 heads of 128: 194 us, 5.5 TB/s; 64 sequences of 1024 to
-// 4096 tokens with up to 5 new ones: 70 us, 4.1 TB/s.
+// 4096 tokens with up to 5 new ones: 66 us, 4.3 TB/s.
 template <int D, bool BF, int MT>
-__global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
+__device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p, float* joined, float* joined_ml,
+                                            typename Elem<BF>::vec* queries) {
   using E = Elem<BF>;
   using vec = typename E::vec;
   using one = typename E::one;
@@ -308,15 +309,10 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
   constexpr int kTiles = D / 16;       // accumulator tiles over d
   constexpr int kPad = D + 4;
   constexpr int NW = 4;  // waves
-  __shared__ __align__(16) float joined[NW * 16 * kPad];
-  __shared__ float joined_ml[NW * 16 * 2];
-  __shared__ __align__(16) vec queries[MT * kSteps * 64];  // the same for all four waves: LDS spares their registers
 
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int split = blockIdx.y;
-  Place p;
-  if (!attend_place(a, 16 * MT, lane, p)) return;
   const int row0 = p.tile * 16 * MT, h = p.h;
   const int lim_lo = seen_by(a, p, row0), lim_hi = seen_by(a, p, row0 + 16 * MT - 1);
   const int tiles = lim_hi > 0 ? (lim_hi + 63) >> 6 : 0;
@@ -498,6 +494,23 @@ __global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
       }
     }
   }
+}
+
+// A sequence that fills fewer of the row tiles than the batch's most multiplies as many as it fills (64 sequences of 2000 tokens with
+// up to 6 new ones, 8 query heads a cache head: 70 us, 90 with all tiles; 64 x up to 4096 with up to 5: 66 and 71).
+template <int D, bool BF, int MT>
+__global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
+  __shared__ __align__(16) float joined[4 * 16 * (D + 4)];
+  __shared__ float joined_ml[4 * 16 * 2];
+  __shared__ __align__(16) typename Elem<BF>::vec queries[MT * D / 32 * 64];  // the same for all four waves: LDS spares their registers
+  Place p;
+  if (!attend_place(a, 16 * MT, threadIdx.x & 63, p)) return;
+  if (MT > 1 && p.rows <= 16)
+    attend_rows<D, BF, 1>(a, p, joined, joined_ml, queries);
+  else if (MT > 2 && p.rows <= 32)
+    attend_rows<D, BF, 2>(a, p, joined, joined_ml, queries);
+  else
+    attend_rows<D, BF, MT>(a, p, joined, joined_ml, queries);
 }
 
 // Many rows: the four waves take different rows (MT tiles of 16 each) against the same tiles of 64 tokens, which go through
@@ -801,7 +814,7 @@ AttendPlan attend_plan(const CacheView& c, int64_t T, int64_t S, int64_t width, 
   //   more pairs take six a CU, so that unlike lengths even out (16 x up to 30000, a quarter up: 1536 workgroups 77 us, 768 98,
   //   512 96; all of 30000: 193, 197, 177; 32 x up to 8192: 46, 55, 58).
   // Many rows: two workgroups a CU, and only where that leaves half of them idle.
-  const int resident = c.d * p.mt <= 64 ? 4 : c.d * p.mt <= 128 ? 3 : c.d <= 128 && p.mt == 2 ? 2 : 1;
+  const int resident = p.mt == 1 ? (c.d <= 64 ? 4 : c.d <= 128 ? 3 : 1) : c.d <= 128 && p.mt == 2 ? 2 : 1;
   int64_t splits;
   if (p.wide) {
     splits = 512 / base;
