@@ -8,11 +8,15 @@
 // first product are, lane by lane, the second's operand: lane (m, g) = (lane & 15, lane >> 4) holds row m's scores of
 // the 16 tokens of unit g in both.  Codes go from memory to registers (16 bytes of a key chunk or of a value's
 // 16 tokens), are widened (exactly: bf16 or f16 keys, f16 values) and feed the matrix cores: straight from the registers
-// for few rows, through LDS for many (the two kernels below).  One pass with a running maximum: with t = s log2(e) + ve, in the frame M = max t,
-//   p = 2^(t - M) <= 1 carries the value's scale (so f16 holds the terms that matter, whatever the pages' scales),
-//   l = sum p 2^-ve the softmax's sum in the same frame, out = sum p code / l.
-// (c_g = scale log2(e) 2^ke is the lane's, so t is one fused multiply-add.)  Exponents lie in [-40, 40]: a term that the
-// frame loses (below 2^-126) has less than 2^-46 of the largest weight.
+// for few rows, through LDS for many (the two kernels below).  One pass with a running maximum: with t = s log2(e) + ve, in the
+// frame M = max t so far,
+//   p = 2^(t - M + kLift) <= 2^15 carries the value's scale,
+//   l = sum p 2^-ve the softmax's sum in the same frame (fp32), out = sum p code / l.
+// (c_g = scale log2(e) 2^ke is the lane's, so t is one fused multiply-add.)
+// The matrix cores take p in f16, which holds 11 bits of it down to 2^-14: 2^-29 of the largest.  Smaller ones matter where a
+// token leads by far and holds small values, or a page has a larger scale.  In a tile that has some, what f16 drops of them goes
+// through a product of its own in a frame of its own (left_of_low), so that a weight is off by at most 2^-11 of itself and 2^-79
+// of the row's largest.  Exponents lie in [-40, 40]: a term that l loses (below 2^-126) has less than 2^-61 of the largest weight.
 #include "cache.h"
 
 #include <math.h>
@@ -24,6 +28,7 @@ namespace {
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -206,15 +211,17 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const Place& p
   }
 }
 
-// The weights of 64 tokens from their scores: p = 2^(t - M) in f16, the normaliser, and by how much what was summed before
-// shrinks (returns whether it does).  All of a lane's scores are of one unit, so its page's scales are one factor
-// and one addend (c_g >= 0, ve_g), and the maximum can be taken of the products themselves.  M follows the maximum
-// only when some row's has grown by more than 2^kSlack: p stays far inside f16, and the sums are rescaled once or twice in
-// all instead of whenever one of the rows finds a larger score.  upto[r]: the unit's tokens that row r sees.
-constexpr float kSlack = 8.0f;
+// The weights of 64 tokens from their scores: raise_frame sets the frame M, weigh takes the weights in it.  All of a lane's
+// scores are of one unit, so its page's scales are one factor and one addend (c_g >= 0, ve_g), and the extremes can be taken of
+// the products themselves.  upto[r]: the unit's tokens that row r sees.
+//
+// The frame follows the maximum whenever some row of the wave finds a larger one, a few times in a sequence: by alpha, what was
+// summed before shrinks (returns whether it does).  A frame that lags leaves f16 less range below (at 2^4, 4 x up to 1024 new of up
+// to 5000 tokens take 298 us, 252 without: one tile in a few has low weights).
+constexpr float kLift = 15.0f;
 template <int MT, bool MASKED>
-__device__ __forceinline__ bool weigh(const f32x4 (&sc)[4][MT], float c_g, float ve_g, float inv_v, const int (&upto)[MT],
-                                      float (&M)[MT], float (&l)[MT], float (&alpha)[MT], f16x8 (&pf)[MT][2]) {
+__device__ __forceinline__ bool raise_frame(const f32x4 (&sc)[4][MT], float c_g, float ve_g, const int (&upto)[MT], float (&M)[MT],
+                                            float (&l)[MT], float (&alpha)[MT]) {
   float top[MT];
   bool grown = false;
 #pragma unroll
@@ -225,7 +232,7 @@ __device__ __forceinline__ bool weigh(const f32x4 (&sc)[4][MT], float c_g, float
 #pragma unroll
       for (int i = 0; i < 4; ++i) mx = fmaxf(mx, !MASKED || 4 * tt + i < upto[r] ? sc[tt][r][i] : -INFINITY);
     top[r] = row_max4(mx == -INFINITY ? mx : fmaf(mx, c_g, ve_g));
-    grown |= top[r] > M[r] + kSlack;
+    grown |= top[r] > M[r];
   }
   grown = __ballot(grown) != 0;
   if (grown) {
@@ -237,9 +244,18 @@ __device__ __forceinline__ bool weigh(const f32x4 (&sc)[4][MT], float c_g, float
       M[r] = to;
     }
   }
+  return grown;
+}
+__device__ __forceinline__ float weight_offset(float ve_g, float M) { return ve_g + kLift - (M == -INFINITY ? 0.0f : M); }
+
+// Returns whether some visible weight lies below f16's normal range (from the weights' bits: they are not negative).
+template <int MT, bool MASKED>
+__device__ __forceinline__ bool weigh(const f32x4 (&sc)[4][MT], float c_g, float ve_g, float inv_v, const int (&upto)[MT],
+                                      const float (&M)[MT], float (&l)[MT], f16x8 (&pf)[MT][2]) {
+  u16x2 least = {0x3c00, 0x3c00};
 #pragma unroll
   for (int r = 0; r < MT; ++r) {
-    const float off = ve_g - (M[r] == -INFINITY ? 0.0f : M[r]);
+    const float off = weight_offset(ve_g, M[r]);
     float sum = 0.0f;
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt)
@@ -251,8 +267,61 @@ __device__ __forceinline__ bool weigh(const f32x4 (&sc)[4][MT], float c_g, float
         pf[r][tt >> 1][4 * (tt & 1) + i] = (_Float16)p;
       }
     l[r] = fmaf(sum, inv_v, l[r]);
+#pragma unroll
+    for (int j = 0; j < 16; j += 2) {
+      const f16x2 two = {pf[r][j >> 3][j & 7], pf[r][j >> 3][(j & 7) + 1]};
+      u16x2 bits = __builtin_bit_cast(u16x2, two);
+      if (MASKED) bits = u16x2{j < upto[r] ? bits[0] : (uint16_t)0x3c00, j + 1 < upto[r] ? bits[1] : (uint16_t)0x3c00};
+      least = __builtin_elementwise_min(least, bits);
+    }
   }
-  return grown;
+  return __ballot(min(least[0], least[1]) < 0x0400) != 0;
+}
+
+// What f16 does not hold of a row tile's weights below its normal range, p - f16(p), as f16 in a frame of its own: times a power
+// of two that brings the row's largest to 2^14 .. 2^15; back: what brings a sum of them into the frame M again.
+template <int MT>
+__device__ __forceinline__ void left_of_low(const f32x4 (&sc)[4][MT], int r, float c_g, float ve_g, int upto, float M, f16x8 (&left)[2],
+                                            float& back) {
+  __builtin_amdgcn_sched_barrier(0);
+  float off = weight_offset(ve_g, M);
+  asm volatile("" : "+v"(off));  // (weights computed here are not held for weigh)
+  const auto weight = [&](int tt, int i) {  // (as in weigh)
+    const float p = __builtin_amdgcn_exp2f(fmaf(sc[tt][r][i], c_g, off));
+    return 4 * tt + i < upto && p < 0x1p-14f ? p : 0.0f;
+  };
+  float most = 0.0f;
+#pragma unroll
+  for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = fmaxf(most, weight(tt, i));
+  // (what is left of a weight of 2^-24 or more is at most 2^-25)
+  most = fminf(fmaxf(row_max4(most), 0x1p-110f), 0x1p-25f);
+  const uint32_t octave = __builtin_bit_cast(uint32_t, most) & 0x7f800000u;
+  const float up = __builtin_bit_cast(float, 0x7f000000u - octave) * 0x1p14f;
+  back = __builtin_bit_cast(float, octave) * 0x1p-14f;
+#pragma unroll
+  for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float p = weight(tt, i);
+      left[tt >> 1][4 * (tt & 1) + i] = (_Float16)((p - (float)(_Float16)p) * up);
+    }
+}
+
+// Adds what is left of a row tile's low weights to its sums: v(dt, half) are the tile's values as operands.  Tiles that have such
+// weights are rare, so this takes one accumulator after the other, in few registers.
+template <int MT, int TILES, typename Values>
+__device__ __forceinline__ void add_left(const f16x8 (&left)[2], float back, int r, f32x4 (&acc)[TILES][MT], Values values) {
+#pragma unroll
+  for (int dt = 0; dt < TILES; ++dt) {
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int hs = 0; hs < 2; ++hs) sum = Elem<false>::mfma(values(dt, hs), left[hs], sum);
+    acc[dt][r] = __builtin_elementwise_fma(sum, f32x4{back, back, back, back}, acc[dt][r]);
+  }
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // A NaN code among tokens that only some rows see must reach those rows alone: it is taken out of the values (a lane's 16
@@ -297,6 +366,7 @@ __device__ __forceinline__ void add_values(const f16x8 (&v)[2], const f16x8 (&pf
 // to registers, and join at the end.  Bound by memory: a tile's keys are loaded while the one before is
 // weighed, its values while its keys are multiplied.  4 x 131072 tokens, 8 heads of 128: 194 us, 5.5 TB/s; 64 sequences of 1024 to
 // 4096 tokens with up to 5 new ones: 66 us, 4.3 TB/s.
+constexpr int joined_part(int D, int MT) { return 16 * (D + 4) > 576 * MT ? 16 * (D + 4) : 576 * MT; }  // floats of a wave
 template <int D, bool BF, int MT>
 __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p, float* joined, float* joined_ml,
                                             typename Elem<BF>::vec* queries) {
@@ -343,6 +413,14 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
     for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
+  // the wave's part of `joined`: what is left of low weights during the tokens, its sums after them
+  float* const part = joined + wave * joined_part(D, MT);
+  const auto opaque_lane = [&]() {  // (for addresses of the rare tiles with low weights, which no register holds for the others)
+    int at = lane;
+    asm volatile("" : "+v"(at));
+    return at;
+  };
+
   const int t0 = t_begin + wave;
   const PageWalk walk(a, p);
   u32x4 kc[4][kWhole];
@@ -385,7 +463,8 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
             sc[tt][r] = E::mfma(kf, qf[r], st == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sc[tt][r]);
         }
       }
-      const float c_g = a.scale_log2 * pow2i(ke), ve_g = (float)ve, inv_v = pow2i(-ve);
+      float c_g = a.scale_log2 * pow2i(ke), ve_g = (float)ve, inv_v = pow2i(-ve);
+      asm volatile("" : "+v"(c_g), "+v"(ve_g), "+v"(inv_v));  // (before the next tile's exponents are loaded, into the same registers)
       const bool ok_now = ok;
       // the next tile's keys, exponents, and the page ids after it
       __builtin_amdgcn_sched_barrier(0);  // (into the registers of this one's)
@@ -402,37 +481,63 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
       int upto[MT];
 #pragma unroll
       for (int r = 0; r < MT; ++r) upto[r] = ok_now ? lim[r] - first : 0;
-      f16x8 pf[MT][2];
       float alpha[MT];
-      const bool grown = masked ? weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, alpha, pf)
-                                : weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, alpha, pf);
+      bool grown = masked ? raise_frame<MT, true>(sc, c_g, ve_g, upto, M, l, alpha)
+                          : raise_frame<MT, false>(sc, c_g, ve_g, upto, M, l, alpha);
+      f16x8 pf[MT][2];
+      const bool low = masked ? weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf)
+                              : weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+      if (__builtin_expect(low, 0)) {
+#pragma unroll
+        for (int r = 0; r < MT; ++r) {
+          f16x8 left[2];
+          float back;
+          left_of_low<MT>(sc, r, c_g, ve_g, upto[r], M[r], left, back);
+          const int at = opaque_lane();
+          reinterpret_cast<f16x8*>(part)[128 * r + at] = left[0];
+          reinterpret_cast<f16x8*>(part)[128 * r + 64 + at] = left[1];
+          part[512 * MT + 64 * r + at] = back;
+        }
+      }
       if (grown) {
 #pragma unroll
         for (int r = 0; r < MT; ++r)
 #pragma unroll
           for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] *= alpha[r];
       }
-      // what lies past the sequence's end is not the cache's: any bytes
-      const int keep = ok_now ? min(max(p.len - first, 0), 16) : 0;
-      bool bad = false;
       if (masked) {
+        // what lies past the sequence's end is not the cache's: any bytes
+        const int keep = ok_now ? min(max(p.len - first, 0), 16) : 0;
         uint32_t any = 0;
 #pragma unroll
-        for (int dt = 0; dt < kTiles; ++dt) any |= nan_any(vc[dt]);
-        bad = __ballot(any != 0) != 0;
+        for (int dt = 0; dt < kTiles; ++dt) {
+          vc[dt] = low_bytes(vc[dt], keep);
+          any |= nan_any(vc[dt]);
+        }
+        if (__ballot(any != 0) != 0) {
+#pragma unroll
+          for (int dt = 0; dt < kTiles; ++dt) {
+            mark_nan<MT>(vc[dt], upto, acc[dt]);
+            vc[dt] = nan_out(vc[dt]);
+          }
+        }
       }
 #pragma unroll
       for (int dt = 0; dt < kTiles; ++dt) {
-        u32x4 c = vc[dt];
-        if (masked) {
-          c = low_bytes(c, keep);
-          if (bad) {
-            mark_nan<MT>(c, upto, acc[dt]);
-            c = nan_out(c);
-          }
-        }
-        const f16x8 v[2] = {Elem<false>::widen(c[0], c[1]), Elem<false>::widen(c[2], c[3])};
+        const f16x8 v[2] = {Elem<false>::widen(vc[dt][0], vc[dt][1]), Elem<false>::widen(vc[dt][2], vc[dt][3])};
         add_values<MT>(v, pf, acc[dt]);
+      }
+      if (__builtin_expect(low, 0)) {
+#pragma unroll
+        for (int r = 0; r < MT; ++r) {
+          const int from = opaque_lane();
+          const f16x8 left[2] = {reinterpret_cast<f16x8*>(part)[128 * r + from], reinterpret_cast<f16x8*>(part)[128 * r + 64 + from]};
+          add_left<MT, kTiles>(left, part[512 * MT + 64 * r + from], r, acc, [&](int dt, int hs) {
+            uint32_t lo = vc[dt][2 * hs], hi = vc[dt][2 * hs + 1];
+            asm volatile("" : "+v"(lo), "+v"(hi));  // widened here, not held from before
+            return Elem<false>::widen(lo, hi);
+          });
+        }
       }
     }
   }
@@ -446,7 +551,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
 #pragma unroll
   for (int r = 0; r < MT; ++r) {
     if (r > 0) __syncthreads();
-    float* w = joined + (wave * 16 + m) * kPad + 4 * g;
+    float* w = part + m * kPad + 4 * g;
 #pragma unroll
     for (int dt = 0; dt < kTiles; ++dt) *reinterpret_cast<f32x4*>(w + 16 * dt) = acc[dt][r];
     if (g == 0) {
@@ -472,7 +577,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
         f32x2 o = {0.0f, 0.0f};
 #pragma unroll
         for (int w4 = 0; w4 < NW; ++w4) {
-          const f32x2 x = *reinterpret_cast<const f32x2*>(joined + (w4 * 16 + jr) * kPad + jd + e);
+          const f32x2 x = *reinterpret_cast<const f32x2*>(joined + w4 * joined_part(D, MT) + jr * kPad + jd + e);
           o[0] = fmaf(wgt[w4], x[0], o[0]);
           o[1] = fmaf(wgt[w4], x[1], o[1]);
         }
@@ -486,7 +591,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
       }
       if (jd == 0) {
         if (a.splits == 1) {
-          if (a.lse) a.lse[id] = lsum == 0.0f ? -INFINITY : (top + log2f(lsum)) * 0.693147180559945f;
+          if (a.lse) a.lse[id] = lsum == 0.0f ? -INFINITY : ((top - kLift) + log2f(lsum)) * 0.693147180559945f;
         } else {
           a.part_ml[2 * (id * a.splits + split)] = top;
           a.part_ml[2 * (id * a.splits + split) + 1] = lsum;
@@ -499,8 +604,8 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
 // A sequence that fills fewer of the row tiles than the batch's most multiplies as many as it fills (64 sequences of 2000 tokens with
 // up to 6 new ones, 8 query heads a cache head: 70 us, 90 with all tiles; 64 x up to 4096 with up to 5: 66 and 71).
 template <int D, bool BF, int MT>
-__global__ __launch_bounds__(256) void attend_kernel(const AttendArgs a) {
-  __shared__ __align__(16) float joined[4 * 16 * (D + 4)];
+__global__ __launch_bounds__(256, D <= 128 && MT <= 2 ? 2 : 1) void attend_kernel(const AttendArgs a) {
+  __shared__ __align__(16) float joined[4 * joined_part(D, MT)];
   __shared__ float joined_ml[4 * 16 * 2];
   __shared__ __align__(16) typename Elem<BF>::vec queries[MT * D / 32 * 64];  // the same for all four waves: LDS spares their registers
   Place p;
@@ -629,7 +734,8 @@ __global__ __launch_bounds__(256, 2) void attend_wide_kernel(const AttendArgs a)
     put(t_begin, ok);
     __syncthreads();
     for (int t = t_begin; t < t_end; ++t) {
-      const float c_g = a.scale_log2 * pow2i(ke), ve_g = (float)ve, inv_v = pow2i(-ve);
+      float c_g = a.scale_log2 * pow2i(ke), ve_g = (float)ve, inv_v = pow2i(-ve);
+      asm volatile("" : "+v"(c_g), "+v"(ve_g), "+v"(inv_v));  // (before the next tile's exponents are loaded, into the same registers)
       const bool ok_now = ok;
       const bool more = t + 1 < t_end;
       if (more) {
@@ -661,10 +767,12 @@ __global__ __launch_bounds__(256, 2) void attend_wide_kernel(const AttendArgs a)
         int upto[MT];
 #pragma unroll
         for (int r = 0; r < MT; ++r) upto[r] = ok_now ? lim[r] - first : 0;
-        f16x8 pf[MT][2];
         float alpha[MT];
-        const bool grown = masked ? weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, alpha, pf)
-                                  : weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, alpha, pf);
+        const bool grown = masked ? raise_frame<MT, true>(sc, c_g, ve_g, upto, M, l, alpha)
+                                  : raise_frame<MT, false>(sc, c_g, ve_g, upto, M, l, alpha);
+        f16x8 pf[MT][2];
+        const bool low = masked ? weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf)
+                                : weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
         if (grown) {
 #pragma unroll
           for (int r = 0; r < MT; ++r)
@@ -683,6 +791,30 @@ __global__ __launch_bounds__(256, 2) void attend_wide_kernel(const AttendArgs a)
         for (int dt = 0; dt < kTiles; ++dt) {
           const f16x8 v[2] = {vt[2 * dt * 64], vt[(2 * dt + 1) * 64]};
           add_values<MT>(v, pf, acc[dt]);
+        }
+        if (__builtin_expect(low, 0)) {
+#pragma unroll
+          for (int r = 0; r < MT; ++r) {
+            f32x4 again[4][1];  // the row tile's scores (not held from before)
+#pragma unroll
+            for (int tt = 0; tt < 4; ++tt) {
+              again[tt][0] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+              for (int st = 0; st < kSteps; ++st) {
+                vec kf = kt[(tt * kSteps + st) * 64];
+                asm volatile("" : "+v"(kf));
+                again[tt][0] = E::mfma(kf, qf[r][st], again[tt][0]);
+              }
+            }
+            f16x8 left[2];
+            float back;
+            left_of_low<1>(again, 0, c_g, ve_g, upto[r], M[r], left, back);
+            add_left<MT, kTiles>(left, back, r, acc, [&](int dt, int hs) {
+              f16x8 v = vt[(2 * dt + hs) * 64];
+              asm volatile("" : "+v"(v));  // read where it is used, not held from before
+              return v;
+            });
+          }
         }
       }
       if (kBuffers == 1) __syncthreads();  // every wave is done with the tile
@@ -712,7 +844,7 @@ __global__ __launch_bounds__(256, 2) void attend_wide_kernel(const AttendArgs a)
         for (int e = 0; e < 4; ++e) w[e] = (one)(ls == 0.0f ? 0.0f : acc[dt][r][e] * inv);
         *reinterpret_cast<one4*>(o + 16 * dt) = w;
       }
-      if (a.lse && g == 0) a.lse[id] = ls == 0.0f ? -INFINITY : (M[r] + log2f(ls)) * 0.693147180559945f;
+      if (a.lse && g == 0) a.lse[id] = ls == 0.0f ? -INFINITY : ((M[r] - kLift) + log2f(ls)) * 0.693147180559945f;
     } else {
       float* o = a.part + (id * a.splits + split) * D + 4 * g;
 #pragma unroll
@@ -780,7 +912,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, in
   for (int e = 0; e < kPer; ++e)
     if (kPer * lane + e < D)
       static_cast<one*>(a.out)[id * D + kPer * lane + e] = (one)(l == 0.0f ? 0.0f : o[e] / l);
-  if (a.lse && lane == 0) a.lse[id] = l == 0.0f ? -INFINITY : (top + log2f(l)) * 0.693147180559945f;
+  if (a.lse && lane == 0) a.lse[id] = l == 0.0f ? -INFINITY : ((top - kLift) + log2f(l)) * 0.693147180559945f;
 }
 
 // How a call is cut: rows a wave holds, whether the waves take different rows, splits of the tokens.
@@ -808,25 +940,26 @@ AttendPlan attend_plan(const CacheView& c, int64_t T, int64_t S, int64_t width, 
   const int64_t full = (T * group + tile_rows - 1) / tile_rows, base = (p.per_seq ? p.slots : full > S ? full : S) * c.heads;
   // Few rows: each split has at least 8 tiles; none below 2048 tokens, where the second launch costs more than the tiles'
   // latency (one sequence: 1024 tokens 12.8 us whole, 16.3 split; 4096 23.7 and 16.7).  As many workgroups as the 256 CUs
-  // hold at a time by the kernels' registers, but where that is three of one row tile:
-  //   up to 32 (sequence, head) pairs take two a CU (4 x 131072 tokens, 8 heads: 512 workgroups 194 us, 768 214, 1536 215), and
-  //   few of them fewer splits, which are joined one after the other (1 x 100000: 32 splits 47 us, 64 51, 96 54);
-  //   more pairs take six a CU, so that unlike lengths even out (16 x up to 30000, a quarter up: 1536 workgroups 77 us, 768 98,
-  //   512 96; all of 30000: 193, 197, 177; 32 x up to 8192: 46, 55, 58).
+  // hold at a time by the kernels' registers, but where that is two of one row tile:
+  //   up to 32 (sequence, head) pairs take a little less than two a CU (4 x 131072 tokens, 8 heads: 448 workgroups 195 us, 512 222,
+  //   768 213, 1536 210; 2 x 131072: 480 106 us, 512 120), and
+  //   few of them fewer splits, which are joined one after the other (1 x 100000: 32 splits 46 us, 40 54);
+  //   more pairs take four a CU, so that unlike lengths even out (16 x up to 30000, a quarter up: 1024 workgroups 73 us, 512 97,
+  //   1536 77; 8 x up to 60000: 1024 79, 1536 87; 32 x up to 8192: 1024 44, 1536 49; all of 30000: 192, 201, 189).
   // Many rows: two workgroups a CU, and only where that leaves half of them idle.
-  const int resident = p.mt == 1 ? (c.d <= 64 ? 4 : c.d <= 128 ? 3 : 1) : c.d <= 128 && p.mt == 2 ? 2 : 1;
+  const int resident = p.mt == 1 ? (c.d <= 64 ? 4 : c.d <= 128 ? 2 : 1) : c.d <= 128 && p.mt == 2 ? 2 : 1;
   int64_t splits;
   if (p.wide) {
     splits = 512 / base;
   } else if (tiles < 32) {
     splits = 1;
-  } else if (p.mt > 1 || resident != 3) {
+  } else if (p.mt > 1 || resident != 2) {
     splits = (256 * resident + base / 2) / base;
   } else if (base > 32) {
-    splits = 1536 / base;
+    splits = 1024 / base;
   } else {
     const int64_t most = base > 8 ? 32 : 256 / base;
-    splits = 512 / base < most ? 512 / base : most;
+    splits = 511 / base < most ? 511 / base : most;
   }
   if (splits > (tiles + 7) / 8) splits = (tiles + 7) / 8;
   if (splits > 128) splits = 128;
