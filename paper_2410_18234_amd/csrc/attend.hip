@@ -81,6 +81,8 @@ struct Elem<false> {
   }
 };
 
+constexpr float kLift = 15.0f;  // p <= 2^kLift
+
 // Maximum / sum over the four lanes (m, 0..3) of a row.
 __device__ __forceinline__ float row_max4(float x) {
   uint32_t u = __builtin_bit_cast(uint32_t, x);
@@ -113,6 +115,15 @@ __device__ __forceinline__ u32x4 low_bytes(u32x4 x, int keep) {
     x[w] = n == 4 ? x[w] : x[w] & ((1u << (8 * n)) - 1u);
   }
   return x;
+}
+
+// The natural log of a row's sum of exp(scale q . k), from its frame and its sum l there.  (l's octave goes to the frame first:
+// the logarithm left is of 0.5 .. 1, where its rounding is small.)
+__device__ __forceinline__ float log_sum(float M, float l) {
+  if (l == 0.0f) return -INFINITY;
+  int octave;
+  const float part = frexpf(l, &octave);
+  return ((M + ((float)octave - kLift)) + log2f(part)) * 0.693147180559945f;
 }
 
 // The frame of two partial sums: their weights, given (M, l) of each; rows without a visible token have M = -inf.
@@ -218,11 +229,15 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const Place& p
 // The frame follows the maximum whenever some row of the wave finds a larger one, a few times in a sequence: by alpha, what was
 // summed before shrinks (returns whether it does).  A frame that lags leaves f16 less range below (at 2^4, 4 x up to 1024 new of up
 // to 5000 tokens take 298 us, 252 without: one tile in a few has low weights).
-constexpr float kLift = 15.0f;
+//
+// t - M + kLift is one fused multiply-add with ve - M + kLift, whose rounding grows with M.  From kFar on (`far`) the frame is one of
+// scores without ve, max s log2(e), and weights are 2^((s log2(e) - M) + (ve + kLift)): the largest score is exact, and equal scores
+// weigh the same whatever their pages.  M is a reference that sums carry, so rows may change from one to the other.
+constexpr float kFar = 65536.0f;
 template <int MT, bool MASKED>
 __device__ __forceinline__ bool raise_frame(const f32x4 (&sc)[4][MT], float c_g, float ve_g, const int (&upto)[MT], float (&M)[MT],
-                                            float (&l)[MT], float (&alpha)[MT]) {
-  float top[MT];
+                                            float (&l)[MT], float (&alpha)[MT], bool& far) {
+  float top[MT], score[MT];
   bool grown = false;
 #pragma unroll
   for (int r = 0; r < MT; ++r) {
@@ -231,13 +246,22 @@ __device__ __forceinline__ bool raise_frame(const f32x4 (&sc)[4][MT], float c_g,
     for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) mx = fmaxf(mx, !MASKED || 4 * tt + i < upto[r] ? sc[tt][r][i] : -INFINITY);
+    score[r] = mx;
     top[r] = row_max4(mx == -INFINITY ? mx : fmaf(mx, c_g, ve_g));
     grown |= top[r] > M[r];
   }
   grown = __ballot(grown) != 0;
   if (grown) {
+    far = false;
 #pragma unroll
     for (int r = 0; r < MT; ++r) {
+      const float to = fmaxf(M[r], top[r]);
+      far |= fabsf(to) > kFar && to > -INFINITY;
+    }
+    far = __ballot(far) != 0;
+#pragma unroll
+    for (int r = 0; r < MT; ++r) {
+      if (far) top[r] = row_max4(score[r] == -INFINITY ? score[r] : score[r] * c_g);
       const float to = fmaxf(M[r], top[r]);
       alpha[r] = M[r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M[r] - to);
       l[r] *= alpha[r];
@@ -247,6 +271,27 @@ __device__ __forceinline__ bool raise_frame(const f32x4 (&sc)[4][MT], float c_g,
   return grown;
 }
 __device__ __forceinline__ float weight_offset(float ve_g, float M) { return ve_g + kLift - (M == -INFINITY ? 0.0f : M); }
+
+// The weight of a far tile's score (fp32: up to 2^55, before the sum takes the value's scale out)
+__device__ __forceinline__ float far_weight(float sc, float c_g, float ve_g, float M) {
+  return __builtin_amdgcn_exp2f((sc * c_g - (M == -INFINITY ? 0.0f : M)) + (ve_g + kLift));
+}
+
+// The sums of a far tile's weights, which leave f16's range: left_of_low takes all of them.
+template <int MT>
+__device__ __forceinline__ void weigh_far(const f32x4 (&sc)[4][MT], float c_g, float ve_g, float inv_v, const int (&upto)[MT],
+                                          const float (&M)[MT], float (&l)[MT], f16x8 (&pf)[MT][2]) {
+#pragma unroll
+  for (int r = 0; r < MT; ++r) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum += 4 * tt + i < upto[r] ? far_weight(sc[tt][r][i], c_g, ve_g, M[r]) : 0.0f;
+    l[r] = fmaf(sum, inv_v, l[r]);
+    pf[r][0] = pf[r][1] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+  }
+}
 
 // Returns whether some visible weight lies below f16's normal range (from the weights' bits: they are not negative).
 template <int MT, bool MASKED>
@@ -279,16 +324,17 @@ __device__ __forceinline__ bool weigh(const f32x4 (&sc)[4][MT], float c_g, float
 }
 
 // What f16 does not hold of a row tile's weights below its normal range, p - f16(p), as f16 in a frame of its own: times a power
-// of two that brings the row's largest to 2^14 .. 2^15; back: what brings a sum of them into the frame M again.
+// of two that brings the row's largest to 2^14 .. 2^15; back: what brings a sum of them into the frame M again.  Of a far
+// tile all of p.
 template <int MT>
-__device__ __forceinline__ void left_of_low(const f32x4 (&sc)[4][MT], int r, float c_g, float ve_g, int upto, float M, f16x8 (&left)[2],
-                                            float& back) {
+__device__ __forceinline__ void left_of_low(const f32x4 (&sc)[4][MT], int r, float c_g, float ve_g, int upto, float M, bool far,
+                                            f16x8 (&left)[2], float& back) {
   __builtin_amdgcn_sched_barrier(0);
   float off = weight_offset(ve_g, M);
   asm volatile("" : "+v"(off));  // (weights computed here are not held for weigh)
   const auto weight = [&](int tt, int i) {  // (as in weigh)
-    const float p = __builtin_amdgcn_exp2f(fmaf(sc[tt][r][i], c_g, off));
-    return 4 * tt + i < upto && p < 0x1p-14f ? p : 0.0f;
+    const float p = far ? far_weight(sc[tt][r][i], c_g, ve_g, M) : __builtin_amdgcn_exp2f(fmaf(sc[tt][r][i], c_g, off));
+    return 4 * tt + i < upto && (far || p < 0x1p-14f) ? p : 0.0f;
   };
   float most = 0.0f;
 #pragma unroll
@@ -296,7 +342,8 @@ __device__ __forceinline__ void left_of_low(const f32x4 (&sc)[4][MT], int r, flo
 #pragma unroll
     for (int i = 0; i < 4; ++i) most = fmaxf(most, weight(tt, i));
   // (what is left of a weight of 2^-24 or more is at most 2^-25)
-  most = fminf(fmaxf(row_max4(most), 0x1p-110f), 0x1p-25f);
+  most = fmaxf(row_max4(most), 0x1p-110f);
+  if (!far) most = fminf(most, 0x1p-25f);
   const uint32_t octave = __builtin_bit_cast(uint32_t, most) & 0x7f800000u;
   const float up = __builtin_bit_cast(float, 0x7f000000u - octave) * 0x1p14f;
   back = __builtin_bit_cast(float, octave) * 0x1p-14f;
@@ -305,7 +352,7 @@ __device__ __forceinline__ void left_of_low(const f32x4 (&sc)[4][MT], int r, flo
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float p = weight(tt, i);
-      left[tt >> 1][4 * (tt & 1) + i] = (_Float16)((p - (float)(_Float16)p) * up);
+      left[tt >> 1][4 * (tt & 1) + i] = (_Float16)((far ? p : p - (float)(_Float16)p) * up);
     }
 }
 
@@ -405,6 +452,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
   }
   f32x4 acc[kTiles][MT];
   float M[MT], l[MT];
+  bool far = false;
 #pragma unroll
   for (int r = 0; r < MT; ++r) {
     M[r] = -INFINITY;
@@ -482,17 +530,21 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
 #pragma unroll
       for (int r = 0; r < MT; ++r) upto[r] = ok_now ? lim[r] - first : 0;
       float alpha[MT];
-      bool grown = masked ? raise_frame<MT, true>(sc, c_g, ve_g, upto, M, l, alpha)
-                          : raise_frame<MT, false>(sc, c_g, ve_g, upto, M, l, alpha);
+      bool grown = masked ? raise_frame<MT, true>(sc, c_g, ve_g, upto, M, l, alpha, far)
+                          : raise_frame<MT, false>(sc, c_g, ve_g, upto, M, l, alpha, far);
       f16x8 pf[MT][2];
-      const bool low = masked ? weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf)
-                              : weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+      bool low = true;
+      if (__builtin_expect(far, 0))
+        weigh_far<MT>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+      else
+        low = masked ? weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf)
+                     : weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
       if (__builtin_expect(low, 0)) {
 #pragma unroll
         for (int r = 0; r < MT; ++r) {
           f16x8 left[2];
           float back;
-          left_of_low<MT>(sc, r, c_g, ve_g, upto[r], M[r], left, back);
+          left_of_low<MT>(sc, r, c_g, ve_g, upto[r], M[r], far, left, back);
           const int at = opaque_lane();
           reinterpret_cast<f16x8*>(part)[128 * r + at] = left[0];
           reinterpret_cast<f16x8*>(part)[128 * r + 64 + at] = left[1];
@@ -591,7 +643,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
       }
       if (jd == 0) {
         if (a.splits == 1) {
-          if (a.lse) a.lse[id] = lsum == 0.0f ? -INFINITY : ((top - kLift) + log2f(lsum)) * 0.693147180559945f;
+          if (a.lse) a.lse[id] = log_sum(top, lsum);
         } else {
           a.part_ml[2 * (id * a.splits + split)] = top;
           a.part_ml[2 * (id * a.splits + split) + 1] = lsum;
@@ -625,7 +677,7 @@ __global__ __launch_bounds__(256, D <= 128 && MT <= 2 ? 2 : 1) void attend_kerne
 // many of matrix instructions): 4 x up to 1024 new of up to 5000 tokens, 32 query heads of 128: 256 us, 730 TFLOP/s.  64 rows a
 // wave would halve the reads but leave one wave a SIMD (382 against 283 us).
 template <int D, bool BF, int MT>
-__global__ __launch_bounds__(256, 2) void attend_wide_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const AttendArgs a) {
   using E = Elem<BF>;
   using vec = typename E::vec;
   using one = typename E::one;
@@ -657,6 +709,7 @@ __global__ __launch_bounds__(256, 2) void attend_wide_kernel(const AttendArgs a)
   load_queries<D, BF, MT>(a, p, row0, m, g, qf, lim);
   f32x4 acc[kTiles][MT];
   float M[MT], l[MT];
+  bool far = false;
 #pragma unroll
   for (int r = 0; r < MT; ++r) {
     M[r] = -INFINITY;
@@ -768,11 +821,15 @@ __global__ __launch_bounds__(256, 2) void attend_wide_kernel(const AttendArgs a)
 #pragma unroll
         for (int r = 0; r < MT; ++r) upto[r] = ok_now ? lim[r] - first : 0;
         float alpha[MT];
-        const bool grown = masked ? raise_frame<MT, true>(sc, c_g, ve_g, upto, M, l, alpha)
-                                  : raise_frame<MT, false>(sc, c_g, ve_g, upto, M, l, alpha);
+        const bool grown = masked ? raise_frame<MT, true>(sc, c_g, ve_g, upto, M, l, alpha, far)
+                                  : raise_frame<MT, false>(sc, c_g, ve_g, upto, M, l, alpha, far);
         f16x8 pf[MT][2];
-        const bool low = masked ? weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf)
-                                : weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+        bool low = true;
+        if (__builtin_expect(far, 0))
+          weigh_far<MT>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+        else
+          low = masked ? weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf)
+                       : weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
         if (grown) {
 #pragma unroll
           for (int r = 0; r < MT; ++r)
@@ -808,7 +865,7 @@ __global__ __launch_bounds__(256, 2) void attend_wide_kernel(const AttendArgs a)
             }
             f16x8 left[2];
             float back;
-            left_of_low<1>(again, 0, c_g, ve_g, upto[r], M[r], left, back);
+            left_of_low<1>(again, 0, c_g, ve_g, upto[r], M[r], far, left, back);
             add_left<MT, kTiles>(left, back, r, acc, [&](int dt, int hs) {
               f16x8 v = vt[(2 * dt + hs) * 64];
               asm volatile("" : "+v"(v));  // read where it is used, not held from before
@@ -844,7 +901,7 @@ __global__ __launch_bounds__(256, 2) void attend_wide_kernel(const AttendArgs a)
         for (int e = 0; e < 4; ++e) w[e] = (one)(ls == 0.0f ? 0.0f : acc[dt][r][e] * inv);
         *reinterpret_cast<one4*>(o + 16 * dt) = w;
       }
-      if (a.lse && g == 0) a.lse[id] = ls == 0.0f ? -INFINITY : ((M[r] - kLift) + log2f(ls)) * 0.693147180559945f;
+      if (a.lse && g == 0) a.lse[id] = log_sum(M[r], ls);
     } else {
       float* o = a.part + (id * a.splits + split) * D + 4 * g;
 #pragma unroll
@@ -912,7 +969,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, in
   for (int e = 0; e < kPer; ++e)
     if (kPer * lane + e < D)
       static_cast<one*>(a.out)[id * D + kPer * lane + e] = (one)(l == 0.0f ? 0.0f : o[e] / l);
-  if (a.lse && lane == 0) a.lse[id] = l == 0.0f ? -INFINITY : ((top - kLift) + log2f(l)) * 0.693147180559945f;
+  if (a.lse && lane == 0) a.lse[id] = log_sum(top, l);
 }
 
 // How a call is cut: rows a wave holds, whether the waves take different rows, splits of the tokens.
