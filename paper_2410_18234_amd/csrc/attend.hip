@@ -997,23 +997,24 @@ AttendPlan attend_plan(const CacheView& c, int64_t T, int64_t S, int64_t width, 
   const int64_t full = (T * group + tile_rows - 1) / tile_rows, base = (p.per_seq ? p.slots : full > S ? full : S) * c.heads;
   // Few rows: each split has at least 8 tiles; none below 2048 tokens, where the second launch costs more than the tiles'
   // latency (one sequence: 1024 tokens 12.8 us whole, 16.3 split; 4096 23.7 and 16.7).  As many workgroups as the 256 CUs
-  // hold at a time by the kernels' registers, but where that is two of one row tile:
+  // hold at a time by the kernels' registers, but where those are of one row tile and d = 96 (three a CU) or 128 (two):
   //   up to 32 (sequence, head) pairs take a little less than two a CU (4 x 131072 tokens, 8 heads: 448 workgroups 195 us, 512 222,
   //   768 213, 1536 210; 2 x 131072: 480 106 us, 512 120), and
   //   few of them fewer splits, which are joined one after the other (1 x 100000: 32 splits 46 us, 40 54);
-  //   more pairs take four a CU, so that unlike lengths even out (16 x up to 30000, a quarter up: 1024 workgroups 73 us, 512 97,
-  //   1536 77; 8 x up to 60000: 1024 79, 1536 87; 32 x up to 8192: 1024 44, 1536 49; all of 30000: 192, 201, 189).
+  //   more pairs take twice what is resident, so that unlike lengths even out (d = 128, 16 x up to 30000, a quarter up: 1024
+  //   workgroups 73 us, 512 97, 1536 77; 8 x up to 60000: 1024 79, 1536 87; 32 x up to 8192: 1024 44, 1536 49; all of 30000: 192,
+  //   201, 189; d = 96, 32 x up to 8192: 1024 44, 1536 39; 16 x up to 30000: 73 and 65).
   // Many rows: two workgroups a CU, and only where that leaves half of them idle.
-  const int resident = p.mt == 1 ? (c.d <= 64 ? 4 : c.d <= 128 ? 2 : 1) : c.d <= 128 && p.mt == 2 ? 2 : 1;
+  const int resident = p.mt == 1 ? (c.d <= 64 ? 4 : c.d <= 96 ? 3 : c.d <= 128 ? 2 : 1) : c.d <= 128 && p.mt == 2 ? 2 : 1;
   int64_t splits;
   if (p.wide) {
     splits = 512 / base;
   } else if (tiles < 32) {
     splits = 1;
-  } else if (p.mt > 1 || resident != 2) {
+  } else if (p.mt > 1 || c.d <= 64 || c.d > 128) {
     splits = (256 * resident + base / 2) / base;
   } else if (base > 32) {
-    splits = 1024 / base;
+    splits = 512 * resident / base;
   } else {
     const int64_t most = base > 8 ? 32 : 256 / base;
     splits = 511 / base < most ? 511 / base : most;
