@@ -511,6 +511,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
             sc[tt][r] = E::mfma(kf, qf[r], st == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sc[tt][r]);
         }
       }
+      if (!ok) ke = ve = 0;  // (no page: page 0 was read in its place, whose exponents may be any byte)
       float c_g = a.scale_log2 * pow2i(ke), ve_g = (float)ve, inv_v = pow2i(-ve);
       asm volatile("" : "+v"(c_g), "+v"(ve_g), "+v"(inv_v));  // (before the next tile's exponents are loaded, into the same registers)
       const bool ok_now = ok;
@@ -787,6 +788,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
     put(t_begin, ok);
     __syncthreads();
     for (int t = t_begin; t < t_end; ++t) {
+      if (!ok) ke = ve = 0;  // (no page: page 0 was read in its place, whose exponents may be any byte)
       float c_g = a.scale_log2 * pow2i(ke), ve_g = (float)ve, inv_v = pow2i(-ve);
       asm volatile("" : "+v"(c_g), "+v"(ve_g), "+v"(inv_v));  // (before the next tile's exponents are loaded, into the same registers)
       const bool ok_now = ok;
