@@ -43,6 +43,7 @@ struct AttendArgs {
   int64_t q_st, q_sh, width, T, pages;
   int S, heads, group, page_shift;
   int per_seq;   // row tiles of a sequence (uniform), 0: found from starts
+  int slot0;     // first row tile of the launch
   int splits, split_tiles;
   float scale_log2;  // |scale| log2(e)
   bool negative;
@@ -156,8 +157,8 @@ struct Place {
 // are a multiple of 8 (workgroups go round the XCDs in order), and find them in its L2.  A sequence's last rows, which see the
 // most tokens, start first (a prompt of 3000 tokens, 64 query heads: 205 us, 246 the other way round).
 __device__ __forceinline__ bool attend_place(const AttendArgs& a, int tile_rows, int lane, Place& p) {
-  const int slot = blockIdx.x / a.heads;
-  p.h = blockIdx.x - slot * a.heads;
+  const int part = blockIdx.x / a.heads, slot = a.slot0 + part;
+  p.h = blockIdx.x - part * a.heads;
   if (a.per_seq > 0) {
     p.s = slot / a.per_seq;
     p.tile = slot - p.s * a.per_seq;
@@ -1031,29 +1032,31 @@ AttendPlan attend_plan(const CacheView& c, int64_t T, int64_t S, int64_t width, 
   return p;
 }
 
-template <int D, bool BF, int MT>
-void attend_few(const AttendArgs& a, int64_t slots, hipStream_t st) {
-  attend_kernel<D, BF, MT><<<dim3((unsigned)(slots * a.heads), (unsigned)a.splits), 256, 0, st>>>(a);
-}
-template <int D, bool BF, int MT>
-void attend_many(const AttendArgs& a, int64_t slots, hipStream_t st) {
-  attend_wide_kernel<D, BF, MT><<<dim3((unsigned)(slots * a.heads), (unsigned)a.splits), 256, 0, st>>>(a);
+// The launches of a call: a dimension of one holds less than 2^32 threads.
+template <typename Kernel>
+void attend_slots(Kernel kernel, AttendArgs a, int64_t slots, hipStream_t st) {
+  const int64_t most = ((1 << 24) - 1) / a.heads;
+  for (int64_t at = 0; at < slots; at += most) {
+    a.slot0 = (int)at;
+    const int64_t n = slots - at < most ? slots - at : most;
+    kernel<<<dim3((unsigned)(n * a.heads), (unsigned)a.splits), 256, 0, st>>>(a);
+  }
 }
 
 template <int D, bool BF>
 hipError_t attend_launch(const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
   if (p.wide) {
-    attend_many<D, BF, D == 256 ? 1 : 2>(a, p.slots, st);
+    attend_slots(attend_wide_kernel<D, BF, D == 256 ? 1 : 2>, a, p.slots, st);
   } else if (p.mt == 1) {
-    attend_few<D, BF, 1>(a, p.slots, st);
+    attend_slots(attend_kernel<D, BF, 1>, a, p.slots, st);
   } else if (p.mt == 2) {
-    attend_few<D, BF, 2>(a, p.slots, st);
+    attend_slots(attend_kernel<D, BF, 2>, a, p.slots, st);
   } else if constexpr (D <= 128) {
-    attend_few<D, BF, 4>(a, p.slots, st);
+    attend_slots(attend_kernel<D, BF, 4>, a, p.slots, st);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t total = a.T * a.heads * a.group;
+  const int64_t total = a.T * a.heads * a.group;  // (at most 2^16: calls of more rows are not split)
   attend_join_kernel<D, BF><<<(unsigned)((total + 3) / 4), 256, 0, st>>>(a, 16 * p.mt, total);
   return hipGetLastError();
 }
