@@ -203,6 +203,16 @@ def _workspace(device: torch.device, nbytes: int) -> torch.Tensor:
     return ws
 
 
+def _ws_arg(dev: torch.device, need: int, workspace: Optional[torch.Tensor]) -> torch.Tensor:
+    """The call's scratch: the caller's, if it is one whole piece of memory of that size."""
+    if workspace is None:
+        return _workspace(dev, need)
+    if (workspace.dtype != torch.uint8 or workspace.device != dev or workspace.numel() < need or
+            not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev} of at least {need} bytes")
+    return workspace
+
+
 def induced_dist(p: torch.Tensor, q: torch.Tensor, K: int, s_max: int = 0, r: Optional[torch.Tensor] = None,
                  row_status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """r [B][V] fp32: distribution of the token picked by importance-weighted selection among K drafts."""
@@ -216,10 +226,7 @@ def induced_dist(p: torch.Tensor, q: torch.Tensor, K: int, s_max: int = 0, r: Op
     need = int(lib.mdss_workspace_bytes(B, V, K, s_max))
     if need == 0 and B > 0:
         _check("mdss_workspace_bytes", 3 if K not in (2, 3) or (K == 3 and not 1 <= s_max <= 4096) else 2)
-    if workspace is None:
-        workspace = _workspace(dev, need)
-    elif workspace.dtype != torch.uint8 or workspace.device != dev or workspace.numel() < need:
-        raise ValueError(f"workspace must be a uint8 tensor on {dev} of at least {need} bytes")
+    workspace = _ws_arg(dev, need, workspace)
     _check("mdss_induced_dist",
            lib.mdss_induced_dist(_ptr(p), _ptr(q), B, V, K, s_max, _ptr(r), _ptr(row_status), _ptr(workspace),
                                  workspace.numel(), _stream(dev)))
@@ -379,10 +386,7 @@ def induced_dist_pair(p: torch.Tensor, q1: torch.Tensor, q2: torch.Tensor, r: Op
     need = int(lib.mdss_workspace_bytes_pair(B, V))
     if need == 0 and B > 0:
         _check("mdss_workspace_bytes_pair", 2)
-    if workspace is None:
-        workspace = _workspace(dev, need)
-    elif workspace.dtype != torch.uint8 or workspace.device != dev or workspace.numel() < need:
-        raise ValueError(f"workspace must be a uint8 tensor on {dev} of at least {need} bytes")
+    workspace = _ws_arg(dev, need, workspace)
     _check("mdss_induced_dist_pair",
            lib.mdss_induced_dist_pair(_ptr(p), _ptr(q1), _ptr(q2), B, V, _ptr(r), _ptr(row_status),
                                       _ptr(workspace), workspace.numel(), _stream(dev)))
@@ -501,10 +505,7 @@ def truncated_lp(p: torch.Tensor, q1: torch.Tensor, q2: Optional[torch.Tensor] =
     need = int(lib.mdss_workspace_bytes_tlp(B, V, tail))
     if need == 0 and B > 0:
         _check("mdss_workspace_bytes_tlp", 1 if tail not in (MDSS_TLP_SORTED, MDSS_TLP_HALF) else 2)
-    if workspace is None:
-        workspace = _workspace(dev, need)
-    elif workspace.dtype != torch.uint8 or workspace.device != dev or workspace.numel() < need:
-        raise ValueError(f"workspace must be a uint8 tensor on {dev} of at least {need} bytes")
+    workspace = _ws_arg(dev, need, workspace)
     _check("mdss_truncated_lp",
            lib.mdss_truncated_lp(_ptr(p), _ptr(q1), _ptr(q2), B, V, s, tail, _ptr(r), _ptr(omega1), _ptr(w),
                                  _ptr(accept), _ptr(row_status), _ptr(workspace), workspace.numel(), _stream(dev)))
@@ -573,10 +574,7 @@ def induced_dist_successive(p: torch.Tensor, q: torch.Tensor, K: int, r_stages: 
     need = int(lib.mdss_workspace_bytes_successive(B, V))
     if need == 0 and B > 0:
         _check("mdss_workspace_bytes_successive", 2)
-    if workspace is None:
-        workspace = _workspace(dev, need)
-    elif workspace.dtype != torch.uint8 or workspace.device != dev or workspace.numel() < need:
-        raise ValueError(f"workspace must be a uint8 tensor on {dev} of at least {need} bytes")
+    workspace = _ws_arg(dev, need, workspace)
     _check("mdss_induced_dist_successive",
            lib.mdss_induced_dist_successive(_ptr(p), _ptr(q), B, V, K, _ptr(r_stages), _ptr(row_status),
                                             _ptr(workspace), workspace.numel(), _stream(dev)))
@@ -642,10 +640,7 @@ def optimal_acceptance(p: torch.Tensor, q: torch.Tensor, K: int = 2, row_status:
     need = int(lib.mdss_workspace_bytes_optimum(B, V))
     if need == 0 and B > 0:
         _check("mdss_workspace_bytes_optimum", 2)
-    if workspace is None:
-        workspace = _workspace(dev, need)
-    elif workspace.dtype != torch.uint8 or workspace.device != dev or workspace.numel() < need:
-        raise ValueError(f"workspace must be a uint8 tensor on {dev} of at least {need} bytes")
+    workspace = _ws_arg(dev, need, workspace)
     pstar = torch.empty(B, dtype=torch.float64, device=dev)
     kstar = torch.empty(B, dtype=torch.int32, device=dev)
     _check("mdss_optimal_acceptance",
@@ -710,14 +705,6 @@ def step_alphabet(p: torch.Tensor, q: torch.Tensor, drafts: torch.Tensor, m: int
     out, kept = alphabet_post(p, pt, mass0, z, u2, seed, offset)
     return {"p_trunc": pt, "mass0": mass0, "r": r, "sel_index": sel_index, "sel_token": sel_token, "z": z,
             "accepted": acc, "out_token": out, "kept": kept, "status": status}
-
-
-def _ws_arg(dev, need: int, workspace: Optional[torch.Tensor]) -> torch.Tensor:
-    if workspace is None:
-        return _workspace(dev, need)
-    if workspace.dtype != torch.uint8 or workspace.device != dev or workspace.numel() < need:
-        raise ValueError(f"workspace must be a uint8 tensor on {dev} of at least {need} bytes")
-    return workspace
 
 
 def workspace_bytes_expsum(B: int, V: int, K: int) -> int:

@@ -19,7 +19,7 @@ from typing import Optional
 
 import torch
 
-from .binding import _check, _need, _ptr, _stream, _workspace, load_library
+from .binding import _check, _need, _ptr, _stream, _ws_arg, load_library
 
 _DTYPES = {torch.bfloat16: 1, torch.float16: 2}
 
@@ -98,11 +98,7 @@ def _status(row_status: Optional[torch.Tensor], S: int, device: torch.device):
 
 
 def _scratch(device: torch.device, need: int, workspace: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
-    if workspace is None:
-        return _workspace(device, need) if need else None
-    if workspace.dtype != torch.uint8 or workspace.device != device or workspace.numel() < need:
-        raise ValueError(f"workspace must be a uint8 tensor on {device} of at least {need} bytes")
-    return workspace
+    return None if workspace is None and not need else _ws_arg(device, need, workspace)
 
 
 def cache_append(cache: PagedCache, layer: int, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor],
