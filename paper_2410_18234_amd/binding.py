@@ -39,7 +39,7 @@ _STATUS = {0: "MDSS_OK", 1: "MDSS_EINVAL", 2: "MDSS_ESHAPE", 3: "MDSS_EUNSUPPORT
 
 _lib = None
 _lock = threading.Lock()
-_ws_cache = {}
+_own = threading.local()  # a host thread's scratch buffers
 
 
 class MdssError(RuntimeError):
@@ -188,18 +188,20 @@ def workspace_bytes(B: int, V: int, K: int, s_max: int = 0) -> int:
 
 
 def _workspace(device: torch.device, nbytes: int) -> torch.Tensor:
-    """Scratch for a call that was given none: one buffer per (device, stream), grown
-    when a call needs more.  A buffer is only ever replaced on its own stream, and the
+    """Scratch for a call that was given none: one buffer per (host thread, device, stream),
+    grown when a call needs more.  A buffer is only ever replaced on its own stream, and the
     caching allocator hands freed memory out again in that stream's order, so work in
     flight on it is never overwritten; calls on other streams have buffers of their
-    own.  Under graph capture every call takes a fresh buffer from the capture's pool."""
+    own, and so have other threads, which may queue launches between those of a call.
+    Under graph capture every call takes a fresh buffer from the capture's pool."""
     if torch.cuda.is_current_stream_capturing():
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    buffers = _own.__dict__
     key = (device, _stream(device))
-    ws = _ws_cache.get(key)
+    ws = buffers.get(key)
     if ws is None or ws.numel() < nbytes:
         ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        _ws_cache[key] = ws
+        buffers[key] = ws
     return ws
 
 

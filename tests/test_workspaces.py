@@ -37,3 +37,30 @@ def test_calls_refuse_it():
     for call in calls:
         with pytest.raises(ValueError):
             call()
+
+
+def test_threads_have_buffers_of_their_own(monkeypatch):
+    """Two host threads on one stream: a call of one may launch between the launches of the other's."""
+    import threading
+    monkeypatch.setattr(binding, "_stream", lambda device: 0)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    both, got = threading.Barrier(2, timeout=20), {}
+
+    def work(i):
+        first = binding._workspace(CPU, 1000)
+        both.wait()
+        again = binding._workspace(CPU, 500)
+        larger = binding._workspace(CPU, 5000)
+        got[i] = (first, again, larger)
+        both.wait()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert got[0][0].data_ptr() != got[1][0].data_ptr() and got[0][2].data_ptr() != got[1][2].data_ptr()
+    for first, again, larger in got.values():  # one thread's calls share a buffer, which grows
+        assert first.data_ptr() == again.data_ptr() and larger.numel() == 5000
+    monkeypatch.setattr(binding, "_stream", lambda device: 1)
+    assert binding._workspace(CPU, 10).data_ptr() == binding._workspace(CPU, 10).data_ptr()
