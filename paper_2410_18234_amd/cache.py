@@ -34,6 +34,9 @@ class PagedCache:
     k      [layers][pages][heads][page_size / 16][head_dim / 16][16][16]  uint8 (unit, 16 of head_dim, token)
     v      [layers][pages][heads][page_size / 16][head_dim][16]           uint8 (unit, head_dim, token)
     k_exp, v_exp [layers][pages][heads]                                   int8; a value is code * 2**exp
+
+    The calls go by the addresses that the tensors had here: the attributes cannot be set anew, and the tensors are not to be
+    given other memory (``set_``, ``resize_``).
     """
 
     __slots__ = ("k", "v", "k_exp", "v_exp", "layers", "pages", "heads", "head_dim", "page_size", "device", "_ref")
@@ -50,11 +53,19 @@ class PagedCache:
         _need(v, "v", torch.uint8, (layers, pages, heads, units, 16 * chunks, 16), device)
         _need(k_exp, "k_exp", torch.int8, (layers, pages, heads), device)
         _need(v_exp, "v_exp", torch.int8, (layers, pages, heads), device)
-        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
-        self.layers, self.pages, self.heads, self.device = layers, pages, heads, device
-        self.head_dim, self.page_size = 16 * chunks, 16 * units
-        self._ref = _DESC.pack(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), pages, layers, heads,
-                               16 * chunks, 16 * units)
+        ref = _DESC.pack(k.data_ptr(), v.data_ptr(), k_exp.data_ptr(), v_exp.data_ptr(), pages, layers, heads,
+                         16 * chunks, 16 * units)
+        for name, x in zip(self.__slots__, (k, v, k_exp, v_exp, layers, pages, heads, 16 * chunks, 16 * units, device, ref)):
+            object.__setattr__(self, name, x)
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"a PagedCache keeps its {name}: make another one of the new tensors")
+
+    def __delattr__(self, name):
+        raise AttributeError(f"a PagedCache keeps its {name}")
+
+    def __reduce__(self):  # copies go by their own tensors' addresses
+        return PagedCache, (self.k, self.v, self.k_exp, self.v_exp)
 
     @classmethod
     def empty(cls, layers: int, pages: int, heads: int, head_dim: int, page_size: int = 64,
