@@ -57,6 +57,8 @@ class Decoder:
 def decode(model, cache, prompts, beams, tokens, eos=-1):
     """Beam search from `prompts` (lists of token ids).  Returns a dict: history [B][beams][tokens] int32, score and done
     [B][beams], and the table, lengths and refs of the beams after the pool's compaction."""
+    if not prompts or not all(prompts):
+        raise ValueError("every prompt must hold a token")
     dev = cache.device
     B, W, ps = len(prompts), beams, cache.page_size
 
