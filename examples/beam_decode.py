@@ -2,7 +2,7 @@
 
 A decoder with random weights.  Prompts of unlike length are appended to the cache and attended over in one ragged call;
 every step then selects continuations, forks the beams' pages (children share their parents' pages, a partly filled one is
-copied when they write to it), and runs the new tokens.  At the end the prompts' pages are freed and the pool is compacted.
+copied when they write to it), and runs the new tokens.  At the end the pool is compacted.
 """
 from __future__ import annotations
 
