@@ -536,11 +536,12 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
                           : raise_frame<MT, false>(sc, c_g, ve_g, upto, M, l, alpha, far);
       f16x8 pf[MT][2];
       bool low = true;
-      if (__builtin_expect(far, 0))
-        weigh_far<MT>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+      if (!(masked || far))
+        low = weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+      else if (!far)
+        low = weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
       else
-        low = masked ? weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf)
-                     : weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+        weigh_far<MT>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
       if (__builtin_expect(low, 0)) {
 #pragma unroll
         for (int r = 0; r < MT; ++r) {
@@ -828,11 +829,12 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
                                   : raise_frame<MT, false>(sc, c_g, ve_g, upto, M, l, alpha, far);
         f16x8 pf[MT][2];
         bool low = true;
-        if (__builtin_expect(far, 0))
-          weigh_far<MT>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+        if (!(masked || far))
+          low = weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+        else if (!far)
+          low = weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
         else
-          low = masked ? weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf)
-                       : weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+          weigh_far<MT>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
         if (grown) {
 #pragma unroll
           for (int r = 0; r < MT; ++r)
