@@ -613,7 +613,10 @@ mdss_status mdss_cache_fork(const mdss_cache* cache, const int32_t* table, const
 /* Moves the used pages to the ids 0 .. used - 1, in all layers: with U pages used,
  * the r-th highest used page >= U goes to the r-th lowest free page < U.
  * table_out (may be table): the rows with the new ids, -1 past a row's tokens;
- * refs_out (not refs): the counts; used [1] int32: U. */
+ * refs_out (not refs): the counts; used [1] int32: U.
+ * What moves goes by refs alone: every table that holds pages of the pool has to follow, so tables of several
+ * holders are passed as rows of one.  Rows that list all ids (of pages * page_size tokens together) come back as the map from
+ * old to new ids, -1 for free pages. */
 size_t mdss_workspace_bytes_cache_compact(const mdss_cache* cache);
 mdss_status mdss_cache_compact(const mdss_cache* cache, const int32_t* table, const int32_t* lengths, int64_t S,
                                int64_t width, const int32_t* refs, int32_t* table_out, int32_t* refs_out,

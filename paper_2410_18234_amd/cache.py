@@ -137,7 +137,7 @@ def cache_attention(q: torch.Tensor, cache: PagedCache, layer: int, starts: Opti
 
     ``scale`` defaults to ``head_dim ** -0.5``.  ``max_new`` and ``max_length`` (0: unknown) say how many new tokens
     and how many tokens a sequence has at most; they only choose how the work is cut.  Returns ``out`` (q's type), or
-    ``(out, lse)`` with ``want_lse``."""
+    ``(out, lse)`` with ``want_lse``; tokens of q that belong to no sequence are not written there."""
     lib = load_library()
     S, width = _rows(cache, starts, table, lengths)
     _tokens(q, "q", cache)
@@ -191,7 +191,10 @@ def cache_fork(cache: PagedCache, table: torch.Tensor, lengths: torch.Tensor, re
 
 def cache_compact(cache: PagedCache, table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor,
                   workspace: Optional[torch.Tensor] = None):
-    """(table, refs, used): the used pages moved to the ids 0 .. used - 1 (``used`` a one-element int32 tensor)."""
+    """(table, refs, used): the used pages moved to the ids 0 .. used - 1 (``used`` a one-element int32 tensor).
+
+    What moves goes by ``refs``: every table that holds pages of the pool has to follow, as rows of this one (rows that
+    list all ids come back as the map from old to new ids, -1 for free pages)."""
     lib = load_library()
     S, width = _rows(cache, None, table, lengths)
     dev = cache.device

@@ -659,7 +659,7 @@ __global__ __launch_bounds__(kThreads) void fork_take_kernel(ForkArgs a, int chu
 }
 
 // Small pools and tables: all but the copies in one workgroup, the counts in LDS (4 x 4 beams of 300 tokens: a call takes
-// 20.5 us against 26.6 with the launches of the large form).
+// 20.1 us against 25.7 with the launches of the large form).
 constexpr int kSmallPages = 8192, kSmallRows = 1024, kSmallEntries = 16384;
 __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(ForkArgs a, int chunks) {
   __shared__ int red[kPlanThreads / 64];
@@ -785,8 +785,8 @@ __device__ __forceinline__ int compact_entry(const CompactArgs& a, int64_t i, Ma
   return to(page);
 }
 
-// Small pools and tables: all but the copies in one workgroup, the counts in LDS (8 rows of 200 tokens: a call takes 19.3 us
-// against 22.3 with the launches of the large form).
+// Small pools and tables: all but the copies in one workgroup, the counts in LDS (8 rows of 200 tokens: a call takes 18.3 us
+// against 21.4 with the launches of the large form).
 __global__ __launch_bounds__(kPlanThreads) void compact_small_kernel(CompactArgs a) {
   __shared__ int red[kPlanThreads / 64];
   __shared__ int32_t refs[kSmallPages], map[kSmallPages], src[kSmallPages / 2], dst[kSmallPages / 2];
