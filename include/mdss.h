@@ -573,7 +573,8 @@ mdss_status mdss_cache_append(const mdss_cache* cache, int32_t layer, const void
  * a sequence's tokens are never seen, whatever they hold, and a NaN in a key or
  * value reaches only the rows that see its token.  Products are of bf16 or f16 (q's
  * type; values and weights f16) with sums, maxima and normalisers in fp32; a weight is off by at most
- * 2^-11 of itself, however small beside the row's largest (and 2^-79 of that one, page scales included).
+ * 2^-11 of itself, and what f16 drops of weights below 2^-29 of the row's largest is added where all of it could
+ * reach 2^-16 of the row's largest element, or where the pages' value exponents are 12 or more apart.
  * max_new and max_length are host-side hints (0: none) on the most new tokens and the largest length
  * of a sequence; they choose how the work is cut and never the result's tokens.
  * heads_q: a multiple of heads, at most 1024 per head, T * heads_q < 2^31.  workspace: at least

@@ -13,10 +13,12 @@
 //   p = 2^(t - M + kLift) <= 2^15 carries the value's scale,
 //   l = sum p 2^-ve the softmax's sum in the same frame (fp32), out = sum p code / l.
 // (c_g = scale log2(e) 2^ke is the lane's, so t is one fused multiply-add.)
-// The matrix cores take p in f16, which holds 11 bits of it down to 2^-14: 2^-29 of the largest.  Smaller ones matter where a
-// token leads by far and holds small values, or a page has a larger scale.  In a tile that has some, what f16 drops of them goes
-// through a product of its own in a frame of its own (left_of_low), so that a weight is off by at most 2^-11 of itself and 2^-79
-// of the row's largest.  Exponents lie in [-40, 40]: a term that l loses (below 2^-126) has less than 2^-61 of the largest weight.
+// The matrix cores take p in f16, which holds 11 bits of it down to 2^-14: 2^-29 of the largest.  Smaller ones matter where the
+// tokens that lead hold values near zero, or a page has a much larger scale: where what f16 drops could reach 2^-16 of a row's
+// largest element (`lacks`) a wave goes over its tokens again (PRECISE), and it goes through a product of its own in a frame of its
+// own (left_of_low).  That costs such a wave more than its first pass; doing it in the one pass, in every tile that has smaller
+// weights, took peaked scores (twice the usual spread, 4 x up to 1024 new of up to 5000 tokens) from 256 to 580 us.  Exponents lie in
+// [-40, 40]: a term that l loses (below 2^-126) has less than 2^-61 of the largest weight.
 #include "cache.h"
 
 #include <math.h>
@@ -83,6 +85,11 @@ struct Elem<false> {
 };
 
 constexpr float kLift = 15.0f;  // p <= 2^kLift
+
+template <bool V>
+struct Flag {
+  static constexpr bool value = V;
+};
 
 // Maximum / sum over the four lanes (m, 0..3) of a row.
 __device__ __forceinline__ float row_max4(float x) {
@@ -155,7 +162,7 @@ struct Place {
 };
 // The head is the fastest index of the grid: the row tiles that read one head's pages run on the same XCD where heads
 // are a multiple of 8 (workgroups go round the XCDs in order), and find them in its L2.  A sequence's last rows, which see the
-// most tokens, start first (a prompt of 3000 tokens, 64 query heads: 205 us, 246 the other way round).
+// most tokens, start first (a prompt of 3000 tokens, 64 query heads: 204 us, 254 the other way round).
 __device__ __forceinline__ bool attend_place(const AttendArgs& a, int tile_rows, int lane, Place& p) {
   const int part = blockIdx.x / a.heads, slot = a.slot0 + part;
   p.h = blockIdx.x - part * a.heads;
@@ -228,14 +235,14 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const Place& p
 // the products themselves.  upto[r]: the unit's tokens that row r sees.
 //
 // The frame follows the maximum whenever some row of the wave finds a larger one, a few times in a sequence: by alpha, what was
-// summed before shrinks (returns whether it does).  A frame that lags leaves f16 less range below (at 2^4, 4 x up to 1024 new of up
-// to 5000 tokens take 298 us, 252 without: one tile in a few has low weights).
+// summed before shrinks (returns whether it does).  A frame that lags would leave f16 less range below.
 //
-// t - M + kLift is one fused multiply-add with ve - M + kLift, whose rounding grows with M.  From kFar on (`far`) the frame is one of
-// scores without ve, max s log2(e), and weights are 2^((s log2(e) - M) + (ve + kLift)): the largest score is exact, and equal scores
-// weigh the same whatever their pages.  M is a reference that sums carry, so rows may change from one to the other.
+// t - M + kLift is one fused multiply-add with ve - M + kLift, whose rounding grows with M.  From kFar on (`far`) the precise frame is
+// one of scores without ve, max s log2(e), and weights are 2^((s log2(e) - M) + (ve + kLift)): the largest score is exact, and equal
+// scores weigh the same whatever their pages.  M is a reference that sums carry, so rows may change from one to the other.
 constexpr float kFar = 65536.0f;
-template <int MT, bool MASKED>
+__device__ __forceinline__ bool is_far(float M) { return fabsf(M) > kFar && M > -INFINITY; }
+template <int MT, bool MASKED, bool PRECISE>
 __device__ __forceinline__ bool raise_frame(const f32x4 (&sc)[4][MT], float c_g, float ve_g, const int (&upto)[MT], float (&M)[MT],
                                             float (&l)[MT], float (&alpha)[MT], bool& far) {
   float top[MT], score[MT];
@@ -254,15 +261,14 @@ __device__ __forceinline__ bool raise_frame(const f32x4 (&sc)[4][MT], float c_g,
   grown = __ballot(grown) != 0;
   if (grown) {
     far = false;
+    if (PRECISE) {
 #pragma unroll
-    for (int r = 0; r < MT; ++r) {
-      const float to = fmaxf(M[r], top[r]);
-      far |= fabsf(to) > kFar && to > -INFINITY;
+      for (int r = 0; r < MT; ++r) far |= is_far(fmaxf(M[r], top[r]));
+      far = __ballot(far) != 0;
     }
-    far = __ballot(far) != 0;
 #pragma unroll
     for (int r = 0; r < MT; ++r) {
-      if (far) top[r] = row_max4(score[r] == -INFINITY ? score[r] : score[r] * c_g);
+      if (PRECISE && far) top[r] = row_max4(score[r] == -INFINITY ? score[r] : score[r] * c_g);
       const float to = fmaxf(M[r], top[r]);
       alpha[r] = M[r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M[r] - to);
       l[r] *= alpha[r];
@@ -294,11 +300,10 @@ __device__ __forceinline__ void weigh_far(const f32x4 (&sc)[4][MT], float c_g, f
   }
 }
 
-// Returns whether some visible weight lies below f16's normal range (from the weights' bits: they are not negative).
+// least: the smallest visible weight so far, by its bits (weights are not negative).
 template <int MT, bool MASKED>
-__device__ __forceinline__ bool weigh(const f32x4 (&sc)[4][MT], float c_g, float ve_g, float inv_v, const int (&upto)[MT],
-                                      const float (&M)[MT], float (&l)[MT], f16x8 (&pf)[MT][2]) {
-  u16x2 least = {0x3c00, 0x3c00};
+__device__ __forceinline__ void weigh(const f32x4 (&sc)[4][MT], float c_g, float ve_g, float inv_v, const int (&upto)[MT],
+                                      const float (&M)[MT], float (&l)[MT], f16x8 (&pf)[MT][2], u16x2& least) {
 #pragma unroll
   for (int r = 0; r < MT; ++r) {
     const float off = weight_offset(ve_g, M[r]);
@@ -321,7 +326,33 @@ __device__ __forceinline__ bool weigh(const f32x4 (&sc)[4][MT], float c_g, float
       least = __builtin_elementwise_min(least, bits);
     }
   }
-  return __ballot(min(least[0], least[1]) < 0x0400) != 0;
+}
+
+// Whether a wave's sums may lack too much: its scores are far; or f16 dropped something of its weights (some lay below its normal
+// range), and pages' scales are 2^kSpread and more apart (what one page has large in some elements may hide another's in the rest), or
+// some row's sums are all small.  `tokens` weights that f16 rounded below 2^-14 are off by tokens 2^-25 448 in all, 2^-16 of a sum
+// that reaches `tokens`.
+constexpr float kSpread = 12.0f;
+template <int MT, int TILES>
+__device__ __forceinline__ bool lacks(const f32x4 (&acc)[TILES][MT], const float (&M)[MT], const int (&lim)[MT], u16x2 least,
+                                      float ve_least, float ve_most, float tokens) {
+  bool far = false;
+#pragma unroll
+  for (int r = 0; r < MT; ++r) far |= is_far(M[r]);
+  if (__ballot(far) != 0) return true;
+  if (__ballot(min(least[0], least[1]) < 0x0400) == 0) return false;
+  if (wave_max(ve_most) + wave_max(-ve_least) >= kSpread) return true;
+  bool small = false;
+#pragma unroll
+  for (int r = 0; r < MT; ++r) {
+    float most = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < TILES; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(acc[dt][r][i]));
+    small |= row_max4(most) < tokens && lim[r] > 0 && M[r] > -INFINITY;
+  }
+  return __ballot(small) != 0;
 }
 
 // What f16 does not hold of a row tile's weights below its normal range, p - f16(p), as f16 in a frame of its own: times a power
@@ -332,7 +363,7 @@ __device__ __forceinline__ void left_of_low(const f32x4 (&sc)[4][MT], int r, flo
                                             f16x8 (&left)[2], float& back) {
   __builtin_amdgcn_sched_barrier(0);
   float off = weight_offset(ve_g, M);
-  asm volatile("" : "+v"(off));  // (weights computed here are not held for weigh)
+  asm volatile("" : "+v"(off));  // (weights computed again, not held from weigh)
   const auto weight = [&](int tt, int i) {  // (as in weigh)
     const float p = far ? far_weight(sc[tt][r][i], c_g, ve_g, M) : __builtin_amdgcn_exp2f(fmaf(sc[tt][r][i], c_g, off));
     return 4 * tt + i < upto && (far || p < 0x1p-14f) ? p : 0.0f;
@@ -357,8 +388,8 @@ __device__ __forceinline__ void left_of_low(const f32x4 (&sc)[4][MT], int r, flo
     }
 }
 
-// Adds what is left of a row tile's low weights to its sums: v(dt, half) are the tile's values as operands.  Tiles that have such
-// weights are rare, so this takes one accumulator after the other, in few registers.
+// Adds what is left of a row tile's low weights to its sums: v(dt, half) are the tile's values as operands (one accumulator after
+// the other, in few registers).
 template <int MT, int TILES, typename Values>
 __device__ __forceinline__ void add_left(const f16x8 (&left)[2], float back, int r, f32x4 (&acc)[TILES][MT], Values values) {
 #pragma unroll
@@ -413,8 +444,8 @@ __device__ __forceinline__ void add_values(const f16x8 (&v)[2], const f16x8 (&pf
 // Few rows: the four waves of a workgroup take the same rows against tiles of 64 tokens in turn, straight from memory
 // to registers, and join at the end.  Bound by memory: a tile's keys are loaded while the one before is
 // weighed, its values while its keys are multiplied.  4 x 131072 tokens, 8 heads of 128: 194 us, 5.5 TB/s; 64 sequences of 1024 to
-// 4096 tokens with up to 5 new ones: 66 us, 4.3 TB/s.
-constexpr int joined_part(int D, int MT) { return 16 * (D + 4) > 576 * MT ? 16 * (D + 4) : 576 * MT; }  // floats of a wave
+// 4096 tokens with up to 5 new ones: 64 us, 4.4 TB/s.
+constexpr int joined_part(int D) { return 16 * (D + 4); }  // floats of a wave
 template <int D, bool BF, int MT>
 __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p, float* joined, float* joined_ml,
                                             typename Elem<BF>::vec* queries) {
@@ -453,28 +484,16 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
   }
   f32x4 acc[kTiles][MT];
   float M[MT], l[MT];
-  bool far = false;
-#pragma unroll
-  for (int r = 0; r < MT; ++r) {
-    M[r] = -INFINITY;
-    l[r] = 0.0f;
-#pragma unroll
-    for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
+  u16x2 least = {0x3c00, 0x3c00};
+  float ve_least = INFINITY, ve_most = -INFINITY;  // of the units' value exponents
 
-  // the wave's part of `joined`: what is left of low weights during the tokens, its sums after them
-  float* const part = joined + wave * joined_part(D, MT);
-  const auto opaque_lane = [&]() {  // (for addresses of the rare tiles with low weights, which no register holds for the others)
-    int at = lane;
-    asm volatile("" : "+v"(at));
-    return at;
-  };
+  float* const part = joined + wave * joined_part(D);  // the wave's sums, after the tokens
 
   const int t0 = t_begin + wave;
   const PageWalk walk(a, p);
   u32x4 kc[4][kWhole];
   u32x2 kh[4];
-  const auto load_k = [&](int page, int t) {
+  const auto load_k = [&](int page, int t) __attribute__((always_inline)) {
     const uint8_t* at = walk.unit(a.k, page, 4 * t + (m >> 2), 16 * D) + (m & 3) * 16;
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) {
@@ -484,13 +503,34 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
     }
   };
 
-  if (t0 < t_end) {
+  const auto pass = [&](auto flag) __attribute__((always_inline)) {
+    constexpr bool PRECISE = decltype(flag)::value;
+#pragma unroll
+    for (int r = 0; r < MT; ++r) {
+      M[r] = -INFINITY;
+      l[r] = 0.0f;
+#pragma unroll
+      for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    if (t0 >= t_end) return;
+    bool far = false;
     bool ok, ok_k;
-    int pk = walk.valid(walk.page(4 * t0 + (m >> 2)), ok_k), pv = walk.valid(walk.page(4 * t0 + g), ok);
-    load_k(pk, t0);
-    int ke = a.k_exp[(int64_t)pv * a.heads + h], ve = a.v_exp[(int64_t)pv * a.heads + h];
-    int pk_next = walk.page(4 * (t0 + NW) + (m >> 2)), pv_next = walk.page(4 * (t0 + NW) + g);
+    int pk, pv, ke, ve;
+    const auto load_tile = [&](int page_k, int page_v, int t) __attribute__((always_inline)) {
+      pk = walk.valid(page_k, ok_k);
+      load_k(pk, t);
+      pv = walk.valid(page_v, ok);
+      ke = a.k_exp[(int64_t)pv * a.heads + h];
+      ve = a.v_exp[(int64_t)pv * a.heads + h];
+    };
+    int pk_next = walk.page(4 * t0 + (m >> 2)), pv_next = walk.page(4 * t0 + g);
+    if (!PRECISE) {
+      load_tile(pk_next, pv_next, t0);
+      pk_next = walk.page(4 * (t0 + NW) + (m >> 2));
+      pv_next = walk.page(4 * (t0 + NW) + g);
+    }
     for (int t = t0; t < t_end; t += NW) {
+      if (PRECISE) load_tile(walk.page(4 * t + (m >> 2)), walk.page(4 * t + g), t);  // (nothing ahead: few registers)
       u32x4 vc[kTiles];
       {
         const uint8_t* at = walk.unit(a.v, pv, 4 * t + g, 16 * D) + m * 16;
@@ -518,13 +558,11 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
       const bool ok_now = ok;
       // the next tile's keys, exponents, and the page ids after it
       __builtin_amdgcn_sched_barrier(0);  // (into the registers of this one's)
-      pk = walk.valid(pk_next, ok_k);
-      load_k(pk, t + NW);
-      pv = walk.valid(pv_next, ok);
-      ke = a.k_exp[(int64_t)pv * a.heads + h];
-      ve = a.v_exp[(int64_t)pv * a.heads + h];
-      pk_next = walk.page(4 * (t + 2 * NW) + (m >> 2));
-      pv_next = walk.page(4 * (t + 2 * NW) + g);
+      if (!PRECISE) {
+        load_tile(pk_next, pv_next, t + NW);
+        pk_next = walk.page(4 * (t + 2 * NW) + (m >> 2));
+        pv_next = walk.page(4 * (t + 2 * NW) + g);
+      }
 
       const bool masked = 64 * (t + 1) > lim_lo || __ballot(ok_now) != ~0ull;
       const int first = 64 * t + 16 * g;  // the lane's first token
@@ -532,27 +570,23 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
 #pragma unroll
       for (int r = 0; r < MT; ++r) upto[r] = ok_now ? lim[r] - first : 0;
       float alpha[MT];
-      bool grown = masked ? raise_frame<MT, true>(sc, c_g, ve_g, upto, M, l, alpha, far)
-                          : raise_frame<MT, false>(sc, c_g, ve_g, upto, M, l, alpha, far);
       f16x8 pf[MT][2];
-      bool low = true;
-      if (!(masked || far))
-        low = weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
-      else if (!far)
-        low = weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
-      else
-        weigh_far<MT>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
-      if (__builtin_expect(low, 0)) {
-#pragma unroll
-        for (int r = 0; r < MT; ++r) {
-          f16x8 left[2];
-          float back;
-          left_of_low<MT>(sc, r, c_g, ve_g, upto[r], M[r], far, left, back);
-          const int at = opaque_lane();
-          reinterpret_cast<f16x8*>(part)[128 * r + at] = left[0];
-          reinterpret_cast<f16x8*>(part)[128 * r + 64 + at] = left[1];
-          part[512 * MT + 64 * r + at] = back;
-        }
+      bool grown;
+      if constexpr (PRECISE) {
+        grown = raise_frame<MT, true, true>(sc, c_g, ve_g, upto, M, l, alpha, far);
+        if (far)
+          weigh_far<MT>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+        else
+          weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf, least);
+      } else {
+        ve_least = fminf(ve_least, ve_g);
+        ve_most = fmaxf(ve_most, ve_g);
+        grown = masked ? raise_frame<MT, true, false>(sc, c_g, ve_g, upto, M, l, alpha, far)
+                       : raise_frame<MT, false, false>(sc, c_g, ve_g, upto, M, l, alpha, far);
+        if (masked)
+          weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf, least);
+        else
+          weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf, least);
       }
       if (grown) {
 #pragma unroll
@@ -582,20 +616,23 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
         const f16x8 v[2] = {Elem<false>::widen(vc[dt][0], vc[dt][1]), Elem<false>::widen(vc[dt][2], vc[dt][3])};
         add_values<MT>(v, pf, acc[dt]);
       }
-      if (__builtin_expect(low, 0)) {
+      if constexpr (PRECISE) {
 #pragma unroll
         for (int r = 0; r < MT; ++r) {
-          const int from = opaque_lane();
-          const f16x8 left[2] = {reinterpret_cast<f16x8*>(part)[128 * r + from], reinterpret_cast<f16x8*>(part)[128 * r + 64 + from]};
-          add_left<MT, kTiles>(left, part[512 * MT + 64 * r + from], r, acc, [&](int dt, int hs) {
+          f16x8 left[2];
+          float back;
+          left_of_low<MT>(sc, r, c_g, ve_g, upto[r], M[r], far, left, back);
+          add_left<MT, kTiles>(left, back, r, acc, [&](int dt, int hs) {
             uint32_t lo = vc[dt][2 * hs], hi = vc[dt][2 * hs + 1];
-            asm volatile("" : "+v"(lo), "+v"(hi));  // widened here, not held from before
+            asm volatile("" : "+v"(lo), "+v"(hi));  // (widened again, not held from above)
             return Elem<false>::widen(lo, hi);
           });
         }
       }
     }
-  }
+  };
+  pass(Flag<false>{});
+  if (t0 < t_end && lacks<MT, kTiles>(acc, M, lim, least, ve_least, ve_most, 64.0f * ((t_end - t0 + NW - 1) / NW))) pass(Flag<true>{});
 
   // join the four waves, 16 rows at a time: thread -> a row and a share of its elements
 #pragma unroll
@@ -632,7 +669,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
         f32x2 o = {0.0f, 0.0f};
 #pragma unroll
         for (int w4 = 0; w4 < NW; ++w4) {
-          const f32x2 x = *reinterpret_cast<const f32x2*>(joined + w4 * joined_part(D, MT) + jr * kPad + jd + e);
+          const f32x2 x = *reinterpret_cast<const f32x2*>(joined + w4 * joined_part(D) + jr * kPad + jd + e);
           o[0] = fmaf(wgt[w4], x[0], o[0]);
           o[1] = fmaf(wgt[w4], x[1], o[1]);
         }
@@ -657,10 +694,10 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
 }
 
 // A sequence that fills fewer of the row tiles than the batch's most multiplies as many as it fills (64 sequences of 2000 tokens with
-// up to 6 new ones, 8 query heads a cache head: 70 us, 90 with all tiles; 64 x up to 4096 with up to 5: 66 and 71).
+// up to 6 new ones, 8 query heads a cache head: 69 us, 84 with all tiles; 64 x up to 4096 with up to 5: 64 and 66).
 template <int D, bool BF, int MT>
-__global__ __launch_bounds__(256, D <= 128 && MT <= 2 ? 2 : 1) void attend_kernel(const AttendArgs a) {
-  __shared__ __align__(16) float joined[4 * joined_part(D, MT)];
+__global__ __launch_bounds__(256, D > 128 || MT > 2 ? 1 : MT == 2 || D > 96 ? 2 : D == 96 ? 3 : 4) void attend_kernel(const AttendArgs a) {
+  __shared__ __align__(16) float joined[4 * joined_part(D)];
   __shared__ float joined_ml[4 * 16 * 2];
   __shared__ __align__(16) typename Elem<BF>::vec queries[MT * D / 32 * 64];  // the same for all four waves: LDS spares their registers
   Place p;
@@ -675,10 +712,10 @@ __global__ __launch_bounds__(256, D <= 128 && MT <= 2 ? 2 : 1) void attend_kerne
 
 // Many rows: the four waves take different rows (MT tiles of 16 each) against the same tiles of 64 tokens, which go through
 // LDS: the next tile's codes are loaded while this one is multiplied, widened once for all four waves, and written for
-// the step after.  A piece of LDS is what one lane multiplies at a time (16 bytes), in the order of the lanes.  Bound by LDS
-// reads and the softmax between the products (d = 128: four waves read 128 KB of LDS a tile, 1024 cycles at 128 bytes, beside as
-// many of matrix instructions): 4 x up to 1024 new of up to 5000 tokens, 32 query heads of 128: 256 us, 730 TFLOP/s.  64 rows a
-// wave would halve the reads but leave one wave a SIMD (382 against 283 us).
+// the step after.  A piece of LDS is what one lane multiplies at a time (16 bytes), in the order of the lanes.  Bound by what a wave
+// does one after the other (two products, the softmax between them, widening): vector instructions take 55 % of a SIMD's
+// cycles, matrix instructions 31 %, and its two waves hardly overlap; LDS is busy for 23 %.  4 x up to 1024 new of up to 5000 tokens,
+// 32 query heads of 128: 256 us, 730 TFLOP/s.  (64 rows a wave leave one wave a SIMD: an earlier form took 382 us so, 283 with 32.)
 template <int D, bool BF, int MT>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const AttendArgs a) {
   using E = Elem<BF>;
@@ -693,6 +730,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
   __shared__ __align__(16) vec key_tile[kBuffers][kKeyVecs * 64];
   __shared__ __align__(16) f16x8 value_tile[kBuffers][2 * kTiles * 64];
   __shared__ int nan_tile[2][4];  // whether a wave took NaN codes out of the values it wrote
+  __shared__ int again_any[4];    // whether a wave's sums lack too much
 
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -712,14 +750,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
   load_queries<D, BF, MT>(a, p, row0, m, g, qf, lim);
   f32x4 acc[kTiles][MT];
   float M[MT], l[MT];
-  bool far = false;
-#pragma unroll
-  for (int r = 0; r < MT; ++r) {
-    M[r] = -INFINITY;
-    l[r] = 0.0f;
-#pragma unroll
-    for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
+  u16x2 least = {0x3c00, 0x3c00};
+  float ve_least = INFINITY, ve_most = -INFINITY;  // of the units' value exponents
 
   const PageWalk walk(a, p);
   u32x4 stage[kEach];
@@ -728,7 +760,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
   constexpr bool kMixed = kKeys % kEach != 0;
   const bool keys = wave * kEach < kKeys;
   const int64_t lane_k = (m & 3) * 16 + g * 256, lane_v = m * 16;
-  const auto load = [&](int pk, int pv, int t) {
+  const auto load = [&](int pk, int pv, int t) __attribute__((always_inline)) {
     const uint8_t* ka = walk.unit(a.k, pk, 4 * t + (m >> 2), 16 * D) + lane_k;
     const uint8_t* va = walk.unit(a.v, pv, 4 * t + g, 16 * D) + lane_v;
     const uint8_t* at = keys ? ka : va;
@@ -743,7 +775,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
     if (kHalf)
       stage_half = *reinterpret_cast<const u32x2*>(ka - g * 256 + wave * 64 + (4 * kWhole + (g >> 1)) * 256 + (g & 1) * 8);
   };
-  const auto put = [&](int t, bool ok) {
+  const auto put = [&](int t, bool ok) __attribute__((always_inline)) {
     const int b = t & (kBuffers - 1);
     if (64 * (t + 1) > p.len || __ballot(ok) != ~0ull) {  // values past the sequence's end are not the cache's: any bytes
       const int keep = ok ? max(p.len - (64 * t + 16 * g), 0) : 0;
@@ -781,7 +813,20 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
     if (kHalf) key_tile[b][(wave * kSteps + kSteps - 1) * 64 + lane] = E::widen(stage_half[0], stage_half[1]);
   };
 
-  if (t_begin < t_end) {
+  // (the precise pass: waves that are content help with the tiles)
+  const auto pass = [&](auto flag, bool mine) __attribute__((always_inline)) {
+    constexpr bool PRECISE = decltype(flag)::value;
+    if (mine) {
+#pragma unroll
+      for (int r = 0; r < MT; ++r) {
+        M[r] = -INFINITY;
+        l[r] = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+    }
+    if (t_begin >= t_end) return;
+    bool far = false;
     bool ok, ok_k;
     int pk = walk.valid(walk.page(4 * t_begin + (m >> 2)), ok_k), pv = walk.valid(walk.page(4 * t_begin + g), ok);
     load(pk, pv, t_begin);
@@ -804,7 +849,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
         pk_next = walk.page(4 * (t + 2) + (m >> 2));
         pv_next = walk.page(4 * (t + 2) + g);
       }
-      if (64 * t < lim_wave) {
+      if (64 * t < lim_wave && mine) {
         const vec* kt = key_tile[t & (kBuffers - 1)] + lane;
         const f16x8* vt = value_tile[t & (kBuffers - 1)] + lane;
         f32x4 sc[4][MT];
@@ -825,16 +870,24 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
 #pragma unroll
         for (int r = 0; r < MT; ++r) upto[r] = ok_now ? lim[r] - first : 0;
         float alpha[MT];
-        const bool grown = masked ? raise_frame<MT, true>(sc, c_g, ve_g, upto, M, l, alpha, far)
-                                  : raise_frame<MT, false>(sc, c_g, ve_g, upto, M, l, alpha, far);
         f16x8 pf[MT][2];
-        bool low = true;
-        if (!(masked || far))
-          low = weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
-        else if (!far)
-          low = weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
-        else
-          weigh_far<MT>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+        bool grown;
+        if constexpr (PRECISE) {
+          grown = raise_frame<MT, true, true>(sc, c_g, ve_g, upto, M, l, alpha, far);
+          if (far)
+            weigh_far<MT>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+          else
+            weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf, least);
+        } else {
+          ve_least = fminf(ve_least, ve_g);
+          ve_most = fmaxf(ve_most, ve_g);
+          grown = masked ? raise_frame<MT, true, false>(sc, c_g, ve_g, upto, M, l, alpha, far)
+                         : raise_frame<MT, false, false>(sc, c_g, ve_g, upto, M, l, alpha, far);
+          if (masked)
+            weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf, least);
+          else
+            weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf, least);
+        }
         if (grown) {
 #pragma unroll
           for (int r = 0; r < MT; ++r)
@@ -854,26 +907,15 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
           const f16x8 v[2] = {vt[2 * dt * 64], vt[(2 * dt + 1) * 64]};
           add_values<MT>(v, pf, acc[dt]);
         }
-        if (__builtin_expect(low, 0)) {
+        if constexpr (PRECISE) {
 #pragma unroll
           for (int r = 0; r < MT; ++r) {
-            f32x4 again[4][1];  // the row tile's scores (not held from before)
-#pragma unroll
-            for (int tt = 0; tt < 4; ++tt) {
-              again[tt][0] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-              for (int st = 0; st < kSteps; ++st) {
-                vec kf = kt[(tt * kSteps + st) * 64];
-                asm volatile("" : "+v"(kf));
-                again[tt][0] = E::mfma(kf, qf[r][st], again[tt][0]);
-              }
-            }
             f16x8 left[2];
             float back;
-            left_of_low<1>(again, 0, c_g, ve_g, upto[r], M[r], far, left, back);
+            left_of_low<MT>(sc, r, c_g, ve_g, upto[r], M[r], far, left, back);
             add_left<MT, kTiles>(left, back, r, acc, [&](int dt, int hs) {
               f16x8 v = vt[(2 * dt + hs) * 64];
-              asm volatile("" : "+v"(v));  // read where it is used, not held from before
+              asm volatile("" : "+v"(v));  // (read again, not held from above)
               return v;
             });
           }
@@ -885,7 +927,13 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
         __syncthreads();
       }
     }
-  }
+  };
+  pass(Flag<false>{}, true);
+  const bool again = 64 * t_begin < lim_wave && t_begin < t_end &&
+                     lacks<MT, kTiles>(acc, M, lim, least, ve_least, ve_most, 64.0f * (t_end - t_begin));
+  if (lane == 0) again_any[wave] = again;
+  __syncthreads();
+  if (again_any[0] | again_any[1] | again_any[2] | again_any[3]) pass(Flag<true>{}, again);
 
   const int64_t heads_q = (int64_t)a.heads * a.group;
 #pragma unroll

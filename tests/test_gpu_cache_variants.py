@@ -86,3 +86,16 @@ def test_calls_repeat_themselves(n, group, length):
     first = mdss.cache_attention(*args).clone()
     for _ in range(5):
         assert (mdss.cache_attention(*args) == first).all()
+
+
+@pytest.mark.parametrize("scale", [0.25, 0.5, 1.0, 4.0, 16.0])
+@pytest.mark.parametrize("n,group", ROWS)
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+def test_scores_of_wide_spread(d, n, group, scale):
+    """Normal keys and queries, scores from 2 to 16 times as far apart as usual and more: from many tokens that count to one."""
+    rng = np.random.default_rng([d, n, int(4 * scale)])
+    lengths = [700, 650]
+    pool = oc.new_pool(1, 45, 1, d, 32)
+    fill(pool, rng)
+    q, q64 = queries(rng, (2 * n, group, d), "f16")
+    run(pool, q, q64, [n, n], lengths, tables(lengths, 32, 45, rng), "f16", uniform=True, scale=scale)
