@@ -162,7 +162,7 @@ struct Place {
 };
 // The head is the fastest index of the grid: the row tiles that read one head's pages run on the same XCD where heads
 // are a multiple of 8 (workgroups go round the XCDs in order), and find them in its L2.  A sequence's last rows, which see the
-// most tokens, start first (a prompt of 3000 tokens, 64 query heads: 204 us, 254 the other way round).
+// most tokens, start first (a prompt of 3000 tokens, 64 query heads: 205 us, 246 the other way round).
 __device__ __forceinline__ bool attend_place(const AttendArgs& a, int tile_rows, int lane, Place& p) {
   const int part = blockIdx.x / a.heads, slot = a.slot0 + part;
   p.h = blockIdx.x - part * a.heads;
@@ -444,7 +444,7 @@ __device__ __forceinline__ void add_values(const f16x8 (&v)[2], const f16x8 (&pf
 // Few rows: the four waves of a workgroup take the same rows against tiles of 64 tokens in turn, straight from memory
 // to registers, and join at the end.  Bound by memory: a tile's keys are loaded while the one before is
 // weighed, its values while its keys are multiplied.  4 x 131072 tokens, 8 heads of 128: 194 us, 5.5 TB/s; 64 sequences of 1024 to
-// 4096 tokens with up to 5 new ones: 64 us, 4.4 TB/s.
+// 4096 tokens with up to 5 new ones: 66 us, 4.3 TB/s.
 constexpr int joined_part(int D) { return 16 * (D + 4); }  // floats of a wave
 template <int D, bool BF, int MT>
 __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p, float* joined, float* joined_ml,
@@ -694,7 +694,8 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
 }
 
 // A sequence that fills fewer of the row tiles than the batch's most multiplies as many as it fills (64 sequences of 2000 tokens with
-// up to 6 new ones, 8 query heads a cache head: 69 us, 84 with all tiles; 64 x up to 4096 with up to 5: 64 and 66).
+// up to 6 new ones, 8 query heads a cache head: 64 us, 77 with all tiles; 64 x up to 4096 with up to 5: 66 and 71).
+// (The bounds are the workgroups a CU that attend_plan counts on: what does not fit the registers then is the precise pass's.)
 template <int D, bool BF, int MT>
 __global__ __launch_bounds__(256, D > 128 || MT > 2 ? 1 : MT == 2 || D > 96 ? 2 : D == 96 ? 3 : 4) void attend_kernel(const AttendArgs a) {
   __shared__ __align__(16) float joined[4 * joined_part(D)];
@@ -713,9 +714,9 @@ __global__ __launch_bounds__(256, D > 128 || MT > 2 ? 1 : MT == 2 || D > 96 ? 2 
 // Many rows: the four waves take different rows (MT tiles of 16 each) against the same tiles of 64 tokens, which go through
 // LDS: the next tile's codes are loaded while this one is multiplied, widened once for all four waves, and written for
 // the step after.  A piece of LDS is what one lane multiplies at a time (16 bytes), in the order of the lanes.  Bound by what a wave
-// does one after the other (two products, the softmax between them, widening): vector instructions take 55 % of a SIMD's
+// does one after the other (two products, the softmax between them, widening): vector instructions take 56 % of a SIMD's
 // cycles, matrix instructions 31 %, and its two waves hardly overlap; LDS is busy for 23 %.  4 x up to 1024 new of up to 5000 tokens,
-// 32 query heads of 128: 256 us, 730 TFLOP/s.  (64 rows a wave leave one wave a SIMD: an earlier form took 382 us so, 283 with 32.)
+// 32 query heads of 128: 252 us, 744 TFLOP/s.  (64 rows a wave leave one wave a SIMD: an earlier form took 382 us so, 283 with 32.)
 template <int D, bool BF, int MT>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const AttendArgs a) {
   using E = Elem<BF>;
@@ -1049,14 +1050,14 @@ AttendPlan attend_plan(const CacheView& c, int64_t T, int64_t S, int64_t width, 
   // (ragged slots are an upper bound: rows that hardly fill their tiles take one a sequence)
   const int64_t full = (T * group + tile_rows - 1) / tile_rows, base = (p.per_seq ? p.slots : full > S ? full : S) * c.heads;
   // Few rows: each split has at least 8 tiles; none below 2048 tokens, where the second launch costs more than the tiles'
-  // latency (one sequence: 1024 tokens 12.8 us whole, 16.3 split; 4096 23.7 and 16.7).  As many workgroups as the 256 CUs
+  // latency (one sequence, the call: 1024 tokens 15 us whole, 19 split; 4096 20.6 and 18.7).  As many workgroups as the 256 CUs
   // hold at a time by the kernels' registers, but where those are of one row tile and d = 96 (three a CU) or 128 (two):
-  //   up to 32 (sequence, head) pairs take a little less than two a CU (4 x 131072 tokens, 8 heads: 448 workgroups 195 us, 512 222,
-  //   768 213, 1536 210; 2 x 131072: 480 106 us, 512 120), and
-  //   few of them fewer splits, which are joined one after the other (1 x 100000: 32 splits 46 us, 40 54);
+  //   up to 32 (sequence, head) pairs take a little less than two a CU (4 x 131072 tokens, 8 heads: 480 workgroups 195 us, 512 224,
+  //   768 214, 1536 212; 2 x 131072: 496 106 us, 512 120), and
+  //   few of them fewer splits, which are joined one after the other (1 x 100000: 32 splits 47 us, 40 55);
   //   more pairs take twice what is resident, so that unlike lengths even out (d = 128, 16 x up to 30000, a quarter up: 1024
-  //   workgroups 73 us, 512 97, 1536 77; 8 x up to 60000: 1024 79, 1536 87; 32 x up to 8192: 1024 44, 1536 49; all of 30000: 192,
-  //   201, 189; d = 96, 32 x up to 8192: 1024 44, 1536 39; 16 x up to 30000: 73 and 65).
+  //   workgroups 73 us, 512 97, 1536 78; 8 x up to 60000: 1024 79, 1536 87; 32 x up to 8192: 1024 45, 1536 49; all of 30000: 192,
+  //   203, 190; d = 96, 32 x up to 8192: 1024 44, 1536 39; 16 x up to 30000: 73 and 65).
   // Many rows: two workgroups a CU, and only where that leaves half of them idle.
   const int resident = p.mt == 1 ? (c.d <= 64 ? 4 : c.d <= 96 ? 3 : c.d <= 128 ? 2 : 1) : c.d <= 128 && p.mt == 2 ? 2 : 1;
   int64_t splits;
