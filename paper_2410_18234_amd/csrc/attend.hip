@@ -1058,6 +1058,8 @@ AttendPlan attend_plan(const CacheView& c, int64_t T, int64_t S, int64_t width, 
   //   more pairs take twice what is resident, so that unlike lengths even out (d = 128, 16 x up to 30000, a quarter up: 1024
   //   workgroups 73 us, 512 97, 1536 78; 8 x up to 60000: 1024 79, 1536 87; 32 x up to 8192: 1024 45, 1536 49; all of 30000: 192,
   //   203, 190; d = 96, 32 x up to 8192: 1024 44, 1536 39; 16 x up to 30000: 73 and 65).
+  // Where the one passes into the other is a choice between equal lengths and unlike ones, which the host does not know: at 32 pairs
+  // 15 splits take 98 us (60000 tokens each) and 96 (up to 100000), 31 splits 102 and 80; at 40 pairs 12 take 118 and 123, 25 124 and 110.
   // Many rows: two workgroups a CU, and only where that leaves half of them idle.
   const int resident = p.mt == 1 ? (c.d <= 64 ? 4 : c.d <= 96 ? 3 : c.d <= 128 ? 2 : 1) : c.d <= 128 && p.mt == 2 ? 2 : 1;
   int64_t splits;
