@@ -628,6 +628,84 @@ mdss_status mdss_cache_compact(const mdss_cache* cache, const int32_t* table, co
  * range are left out. */
 mdss_status mdss_cache_copy(const mdss_cache* cache, const int32_t* src, const int32_t* dst, int64_t n, void* stream);
 
+/* ---- Rotary positions -------------------------------------------------------
+ * A head's first 2 * pairs elements are pairs: (x[i], x[i + pairs]), or
+ * (x[2 i], x[2 i + 1]) where interleaved is not 0; the rest of the head has no
+ * position.  At position t a pair (u, v) becomes
+ *   m (u cos a - v sin a, u sin a + v cos a),   a = t * frequencies[i],  m = magnitude,
+ * and with -a where `inverse` is not 0 (the transposed map: what takes gradients
+ * back).  The angle is formed in fp64 and reduced there; the rest is fp32, rounded
+ * once.  frequencies [pairs] are fp64, radians per position, below 2^16 in size, in device
+ * memory, 8-byte aligned; magnitude in (0, 65536].  1 <= 2 * pairs <= head_dim (else MDSS_ESHAPE). */
+typedef struct mdss_rope {
+  const double* frequencies; /* device pointer */
+  int32_t pairs, interleaved;
+  float magnitude;
+} mdss_rope;                 /* a host struct, read during the call */
+
+/* out[t][h] = x[t][h] at positions[t] ([T] int32), for x [T][heads][head_dim] of
+ * any mdss_dtype; token and head strides in elements, the last dimension
+ * contiguous.  out may be x (with its strides; only the turned part is written
+ * then), else it must not overlap it, and its strides are at least head_dim.
+ * T in [0, 2^24], head_dim up to 65536, heads * head_dim < 2^31.  T = 0: nothing to do. */
+mdss_status mdss_rotary(const void* x, int64_t x_token_stride, int64_t x_head_stride, mdss_dtype dtype, int64_t T, int64_t heads,
+                        int64_t head_dim, const int32_t* positions, const mdss_rope* rope, int32_t inverse, void* out,
+                        int64_t out_token_stride, int64_t out_head_stride, void* stream);
+
+/* mdss_cache_append with the keys turned on the way: from fp32 they are rounded
+ * once, to codes.  positions [T] int32 (nullable: a token's place in its
+ * sequence, lengths[s] - n + i).  The exponent of keys is that of
+ *   max(the largest finite magnitude outside the turned part,
+ *       bound * the largest finite magnitude inside it, before it is turned),
+ * bound = sqrt(2) * magnitude in fp32, which no turned element passes.  A pair
+ * with a NaN or infinity becomes two NaN codes, of either sign.
+ * q [T][heads_q][head_dim] (heads_q 0: none; a multiple of heads, at most 1024 per
+ * head, T * heads_q < 2^31): queries of dtype, which go to q_out (contiguous,
+ * 16-byte aligned, apart from q) turned by the same positions, also for rows
+ * without a page; tokens of no sequence are not written. */
+mdss_status mdss_cache_append_rotary(const mdss_cache* cache, int32_t layer, const void* key, int64_t key_token_stride,
+                                     int64_t key_head_stride, const void* value, int64_t value_token_stride,
+                                     int64_t value_head_stride, mdss_dtype dtype, int64_t T, const int32_t* starts,
+                                     const int32_t* table, int64_t width, const int32_t* lengths, int64_t S,
+                                     const mdss_rope* rope, const int32_t* positions, const void* q, int64_t q_token_stride,
+                                     int64_t q_head_stride, int64_t heads_q, void* q_out, int32_t* row_status, void* stream);
+
+/* ---- Sequences that share a prefix ------------------------------------------
+ * Rows groups[g] .. groups[g + 1] - 1 (groups [G + 1] int32, ascending within
+ * [0, S]) are a group: beams, drafts, or a batch under one instruction.  A row takes
+ * part if it holds at least max(least, 1) tokens before its new ones.  What the group
+ * shares: the leading pages that are the same (and within the pool) in all rows that take
+ * part, up to the fewest tokens that one of them holds before its new ones, in
+ * whole multiples of max(64, page_size); 0 where fewer than two take part or where
+ * that is less than `least`.
+ *   tokens [S]: what row s shares (0: takes no part, or is in no group)
+ *   group_rows [G][4]: the group's first new token and their count (starts of its
+ *   rows; T / S each where starts is NULL), the first row that takes part (-1: none), the
+ *   shared tokens.  (A group whose rows are not within [0, S]: 0, 0, -1, 0.)
+ * G in [0, MDSS_MAX_B], least >= 0. */
+mdss_status mdss_cache_shared(const mdss_cache* cache, int64_t T, const int32_t* starts, const int32_t* table, int64_t width,
+                              const int32_t* lengths, int64_t S, const int32_t* groups, int64_t G, int32_t least,
+                              int32_t* tokens, int32_t* group_rows, void* stream);
+
+/* mdss_cache_attention for such rows, with its results (the same tokens and
+ * weights, joined in another order): a group's new tokens go together over the
+ * tokens it shares, read once from its first row's pages, and each sequence's over
+ * its own.  tokens and group_rows are as mdss_cache_shared writes them for these
+ * starts and tables; they hold for every layer, and as long as the new tokens are as many, tables
+ * keep their leading pages and no length falls.  tokens[s] = 0: the row reads all of its own.
+ * max_new (of a sequence), max_group (new tokens of a group), max_shared and
+ * max_own (a sequence's tokens past the shared ones) are host-side hints on the
+ * most there are (0: none); they choose how the work is cut.
+ * workspace: at least mdss_workspace_bytes_attention_shared(...) bytes, 256-byte aligned. */
+size_t mdss_workspace_bytes_attention_shared(const mdss_cache* cache, int64_t T, int64_t S, int64_t G, int64_t width, int64_t heads_q,
+                                             int32_t uniform, int64_t max_new, int64_t max_group, int64_t max_shared, int64_t max_own);
+mdss_status mdss_cache_attention_shared(const mdss_cache* cache, int32_t layer, const void* q, int64_t q_token_stride,
+                                        int64_t q_head_stride, mdss_dtype dtype, int64_t T, int64_t heads_q,
+                                        const int32_t* starts, const int32_t* table, int64_t width, const int32_t* lengths,
+                                        int64_t S, const int32_t* tokens, const int32_t* group_rows, int64_t G, float scale,
+                                        int64_t max_new, int64_t max_group, int64_t max_shared, int64_t max_own, void* out,
+                                        float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- Beam search ------------------------------------------------------------
  * logits [B][W][V] (any mdss_dtype; rows contiguous, row_stride elements apart),
  * scores [B][W] fp32.  A candidate (w, v) has

@@ -68,8 +68,9 @@ def put_tokens(pool, name, layer, page, head, codes):
         x[...] = codes.reshape(x.shape[0], 16, x.shape[1]).transpose(0, 2, 1)
 
 
-def append(pool, layer, key, value, starts, table, lengths):
-    """key, value [T][H][D] (float64).  Changes the pool; returns the rows without a page."""
+def append(pool, layer, key, value, starts, table, lengths, key_limit=None):
+    """key, value [T][H][D] (float64).  Changes the pool; returns the rows without a page.  key_limit [T][H]: what the
+    keys' exponents go by in place of their magnitudes."""
     ps, pages, H = pool["v"].shape[3] * 16, pool["k"].shape[1], pool["k"].shape[2]
     missing = set()
     for s in range(len(lengths)):
@@ -93,7 +94,10 @@ def append(pool, layer, key, value, starts, table, lengths):
                 for h in range(H):
                     new = np.asarray(x[at:at + m, h], np.float64)
                     mags = np.abs(new[np.isfinite(new)])
-                    e = exponent(float(mags.max()) if mags.size else 0.0)
+                    top = float(mags.max()) if mags.size else 0.0
+                    if name == "k" and key_limit is not None:
+                        top = float(key_limit[at:at + m, h].max())
+                    e = exponent(top)
                     codes = tokens_of(pool, name, layer, page, h).copy()
                     if o:
                         old = int(pool[name + "_exp"][layer, page, h])
@@ -156,6 +160,26 @@ def attention(pool, layer, q, starts, table, lengths, scale):
                     mag[a + i, rows] = (e / z) @ np.abs(vv)
                     slack[a + i, rows] = (np.abs(qq) @ np.abs(kk).T).max(axis=1) * abs(scale)
     return out, lse, mag, slack
+
+
+def shared(pages, ps, starts, table, lengths, groups, least=0):
+    """(tokens [S], group rows [G][4]) of rows groups[g] .. groups[g + 1] - 1; starts [S + 1]."""
+    S, width = table.shape
+    tokens, rows = [0] * S, []
+    for a, b in zip(groups[:-1], groups[1:]):
+        held = {s: min(int(lengths[s]), width * ps) - int(starts[s + 1] - starts[s]) for s in range(a, b)}
+        part = [s for s in range(a, b) if held[s] >= max(1, least)]
+        n = 0
+        if len(part) > 1:
+            while n < width and len({int(table[s, n]) for s in part}) == 1 and 0 <= table[part[0], n] < pages:
+                n += 1
+            unit = max(64, ps)
+            n = min([n * ps] + [held[s] for s in part]) // unit * unit
+            n = n if n >= least else 0
+        for s in part:
+            tokens[s] = n
+        rows.append([int(starts[a]), int(starts[b] - starts[a]), part[0] if part else -1, n])
+    return np.array(tokens, np.int32), np.array(rows, np.int32).reshape(-1, 4)
 
 
 def fork(pool, table, lengths, refs, parent=None, keep=None, grow=None):

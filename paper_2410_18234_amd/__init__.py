@@ -5,8 +5,8 @@ Thin Python binding over the C ABI of ``libmdss.so`` (declared in
 the HIP kernels of the library.  PyTorch supplies device buffers and the
 current HIP stream.
 
-Beside it, a paged 8-bit cache of keys and values (``PagedCache`` and the ``cache_*`` calls) and beam search's step
-(``beam_select``, ``beam_reorder``).
+Beside it, a paged 8-bit cache of keys and values (``PagedCache`` and the ``cache_*`` calls), rotary positions (``Rotary``,
+``rotary``) and beam search's step (``beam_select``, ``beam_reorder``).
 
 Notation: ``p`` = target distribution, ``q`` = draft distribution (the paper
 writes them the other way round), both ``[B][V]`` fp32 on the GPU.
@@ -79,8 +79,16 @@ from .beam import (  # noqa: F401
 from .cache import (  # noqa: F401
     PagedCache,
     cache_append,
+    cache_append_rotary,
     cache_attention,
+    cache_attention_shared,
     cache_compact,
     cache_copy,
     cache_fork,
+    cache_shared,
+)
+from .rotary import (  # noqa: F401
+    Rotary,
+    rotary,
+    rotary_frequencies,
 )

@@ -110,6 +110,13 @@ def load_library():
         lib.mdss_workspace_bytes_attention.argtypes = [P, i64, i64, i64, i64, i32, i64, i64]
         lib.mdss_cache_attention.argtypes = [P, i32, P, i64, i64, i32, i64, i64, P, P, i64, P, i64, ctypes.c_float, i64,
                                              i64, P, P, P, sz, P]
+        lib.mdss_rotary.argtypes = [P, i64, i64, i32, i64, i64, i64, P, P, i32, P, i64, i64, P]
+        lib.mdss_cache_append_rotary.argtypes = [P, i32, P, i64, i64, P, i64, i64, i32, i64, P, P, i64, P, i64, P, P, P, i64, i64,
+                                                 i64, P, P, P]
+        lib.mdss_cache_shared.argtypes = [P, i64, P, P, i64, P, i64, P, i64, i32, P, P, P]
+        lib.mdss_workspace_bytes_attention_shared.argtypes = [P, i64, i64, i64, i64, i64, i32, i64, i64, i64, i64]
+        lib.mdss_cache_attention_shared.argtypes = [P, i32, P, i64, i64, i32, i64, i64, P, P, i64, P, i64, P, P, i64,
+                                                    ctypes.c_float, i64, i64, i64, i64, P, P, P, sz, P]
         lib.mdss_workspace_bytes_cache_fork.argtypes = [P, i64]
         lib.mdss_cache_fork.argtypes = [P, P, P, i64, i64, P, P, P, P, i64, P, P, P, P, P, sz, P]
         lib.mdss_workspace_bytes_cache_compact.argtypes = [P]
@@ -118,10 +125,11 @@ def load_library():
         lib.mdss_workspace_bytes_beam.argtypes = [i64, i64, i64, i64]
         lib.mdss_beam_select.argtypes = [P, i32, i64, P, P, i64, i64, i64, i64, i32, P, P, P, P, P, P, sz, P]
         lib.mdss_beam_reorder.argtypes = [P, P, i64, i64, i64, i64, P, P]
-        for f in ("mdss_workspace_bytes_attention", "mdss_workspace_bytes_cache_fork",
+        for f in ("mdss_workspace_bytes_attention", "mdss_workspace_bytes_attention_shared", "mdss_workspace_bytes_cache_fork",
                   "mdss_workspace_bytes_cache_compact", "mdss_workspace_bytes_beam"):
             getattr(lib, f).restype = sz
-        for f in ("mdss_cache_append", "mdss_cache_attention", "mdss_cache_fork", "mdss_cache_compact",
+        for f in ("mdss_cache_append", "mdss_cache_append_rotary", "mdss_cache_attention", "mdss_cache_attention_shared",
+                  "mdss_cache_shared", "mdss_rotary", "mdss_cache_fork", "mdss_cache_compact",
                   "mdss_cache_copy", "mdss_beam_select", "mdss_beam_reorder"):
             getattr(lib, f).restype = ctypes.c_int
         for f in ("mdss_induced_dist_successive", "mdss_select_successive", "mdss_optimal_acceptance",

@@ -10,6 +10,11 @@ A decoding loop holds a ``PagedCache`` (the pool of pages, for all layers), and 
 
 New tokens are ragged: sequence s owns tokens ``starts[s] .. starts[s + 1] - 1`` of q, k and v (``starts`` None: as
 many for each), the last of its ``lengths[s]`` tokens.
+
+Rows that share their leading pages (beams, drafts, a batch under one instruction) are attended over together:
+
+    shared = cache_shared(cache, T, starts, table, lengths, groups)                      # once a step
+    out = cache_attention_shared(q, cache, layer, starts, table, lengths, shared)        # in every layer
 """
 from __future__ import annotations
 
@@ -20,6 +25,7 @@ from typing import Optional
 import torch
 
 from .binding import _check, _need, _ptr, _stream, _ws_arg, load_library
+from .rotary import Rotary, _rope
 
 _DTYPES = {torch.bfloat16: 1, torch.float16: 2}
 
@@ -129,6 +135,45 @@ def cache_append(cache: PagedCache, layer: int, k: torch.Tensor, v: torch.Tensor
                                  _ptr(row_status), _stream(cache.device)))
 
 
+def cache_append_rotary(cache: PagedCache, layer: int, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor],
+                        table: torch.Tensor, lengths: torch.Tensor, rope: Rotary, positions: Optional[torch.Tensor] = None,
+                        q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                        row_status: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """``cache_append`` with the keys turned on the way, by ``positions [T]`` int32 (None: a token's place in its sequence).
+
+    The queries ``q [T][heads_q][head_dim]``, if given, are turned in the same launch: returned in ``q_out`` (a new tensor if
+    None; never q itself), where tokens of no sequence are not written."""
+    lib = load_library()
+    S, width = _rows(cache, starts, table, lengths)
+    dev = cache.device
+    _tokens(k, "k", cache)
+    _tokens(v, "v", cache, k.dtype)
+    T = k.shape[0]
+    if k.shape[1] != cache.heads or v.shape != k.shape:
+        raise ValueError(f"k and v must be [T][{cache.heads}][{cache.head_dim}]")
+    if positions is not None:
+        _need(positions, "positions", torch.int32, (T,), dev)
+    heads_q = 0
+    if q is not None:
+        _tokens(q, "q", cache, k.dtype)
+        heads_q = q.shape[1]
+        if q.shape[0] != T or heads_q < 1:
+            raise ValueError(f"q must be [{T}][heads_q][{cache.head_dim}]")
+        if q_out is None:
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        else:
+            _need(q_out, "q_out", q.dtype, (T, heads_q, cache.head_dim), dev)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _status(row_status, S, dev)
+    _check("mdss_cache_append_rotary",
+           lib.mdss_cache_append_rotary(cache._ref, layer, _ptr(k), k.stride(0), k.stride(1), _ptr(v), v.stride(0),
+                                        v.stride(1), _DTYPES[k.dtype], T, _ptr(starts), _ptr(table), width, _ptr(lengths), S,
+                                        _rope(rope, dev), _ptr(positions), _ptr(q), q.stride(0) if heads_q else 0,
+                                        q.stride(1) if heads_q else 0, heads_q, _ptr(q_out), _ptr(row_status), _stream(dev)))
+    return q_out
+
+
 def cache_attention(q: torch.Tensor, cache: PagedCache, layer: int, starts: Optional[torch.Tensor],
                     table: torch.Tensor, lengths: torch.Tensor, scale: Optional[float] = None, max_new: int = 0,
                     max_length: int = 0, want_lse: bool = False, out: Optional[torch.Tensor] = None,
@@ -156,6 +201,64 @@ def cache_attention(q: torch.Tensor, cache: PagedCache, layer: int, starts: Opti
                                     1.0 / math.sqrt(cache.head_dim) if scale is None else scale, max_new, max_length,
                                     _ptr(out), _ptr(lse), _ptr(workspace),
                                     workspace.numel() if workspace is not None else 0, _stream(dev)))
+    return (out, lse) if want_lse else out
+
+
+def cache_shared(cache: PagedCache, T: int, starts: Optional[torch.Tensor], table: torch.Tensor, lengths: torch.Tensor,
+                 groups: torch.Tensor, least: int = 0):
+    """(tokens ``[S]``, group_rows ``[G][4]``): what rows ``groups[g] .. groups[g + 1] - 1`` (``groups [G + 1]`` int32, ascending)
+    share, for ``cache_attention_shared``.
+
+    ``T`` new tokens in all.  Rows take part that hold ``least`` tokens (at least one) before their new ones; their shared tokens are the
+    leading pages that are the same in all of them, in whole multiples of ``max(64, page_size)``, 0 where that is less than
+    ``least``.  A group's row: its first new token, its new tokens, its first row that takes part (-1: none), its shared tokens."""
+    lib = load_library()
+    S, width = _rows(cache, starts, table, lengths)
+    dev = cache.device
+    if groups.dim() != 1 or not groups.numel():
+        raise ValueError("groups must be [G + 1]")
+    _need(groups, "groups", torch.int32, tuple(groups.shape), dev)
+    G = groups.numel() - 1
+    tokens = torch.empty_strided((S,), (1,), dtype=torch.int32, device=dev)
+    group_rows = torch.empty_strided((G, 4), (4, 1), dtype=torch.int32, device=dev)
+    _check("mdss_cache_shared",
+           lib.mdss_cache_shared(cache._ref, T, _ptr(starts), _ptr(table), width, _ptr(lengths), S, _ptr(groups), G, least,
+                                 _ptr(tokens), _ptr(group_rows), _stream(dev)))
+    return tokens, group_rows
+
+
+def cache_attention_shared(q: torch.Tensor, cache: PagedCache, layer: int, starts: Optional[torch.Tensor], table: torch.Tensor,
+                           lengths: torch.Tensor, shared, scale: Optional[float] = None, max_new: int = 0, max_group: int = 0,
+                           max_shared: int = 0, max_own: int = 0, want_lse: bool = False, out: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None):
+    """``cache_attention`` that reads what a group of rows shares once for all of them; ``shared`` is what ``cache_shared`` returned
+    for these starts and tables (one result serves every layer, and later steps while tables keep their leading pages).
+
+    ``max_new`` (of a sequence), ``max_group`` (new tokens of a group), ``max_shared`` and ``max_own`` (a sequence's tokens past the
+    shared ones) say how many there are at most (0: unknown); they only choose how the work is cut."""
+    lib = load_library()
+    S, width = _rows(cache, starts, table, lengths)
+    _tokens(q, "q", cache)
+    T, heads_q = q.shape[0], q.shape[1]
+    dev = cache.device
+    tokens, group_rows = shared
+    G = group_rows.shape[0]
+    _need(tokens, "tokens", torch.int32, (S,), dev)
+    _need(group_rows, "group_rows", torch.int32, (G, 4), dev)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    else:
+        _need(out, "out", q.dtype, (T, heads_q, cache.head_dim), dev)
+    lse = torch.empty((T, heads_q), dtype=torch.float32, device=dev) if want_lse else None
+    need = lib.mdss_workspace_bytes_attention_shared(cache._ref, T, S, G, width, heads_q, starts is None, max_new, max_group,
+                                                     max_shared, max_own)
+    workspace = _scratch(dev, need, workspace)
+    _check("mdss_cache_attention_shared",
+           lib.mdss_cache_attention_shared(cache._ref, layer, _ptr(q), q.stride(0), q.stride(1), _DTYPES[q.dtype], T, heads_q,
+                                           _ptr(starts), _ptr(table), width, _ptr(lengths), S, _ptr(tokens), _ptr(group_rows), G,
+                                           1.0 / math.sqrt(cache.head_dim) if scale is None else scale, max_new, max_group,
+                                           max_shared, max_own, _ptr(out), _ptr(lse), _ptr(workspace),
+                                           workspace.numel() if workspace is not None else 0, _stream(dev)))
     return (out, lse) if want_lse else out
 
 

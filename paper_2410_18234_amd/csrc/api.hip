@@ -71,6 +71,24 @@ mdss_status check_tokens(int64_t T, int64_t S, bool uniform) {
   return MDSS_OK;
 }
 
+mdss_status check_rope(const mdss_rope* r, int64_t head_dim) {
+  if (!r) return MDSS_EINVAL;
+  if (head_dim < 1 || r->pairs < 1 || 2 * (int64_t)r->pairs > head_dim) return MDSS_ESHAPE;
+  if (!(r->magnitude > 0.0f) || r->magnitude > 65536.0f || (reinterpret_cast<uintptr_t>(r->frequencies) & 7)) return MDSS_EINVAL;
+  return MDSS_OK;
+}
+
+mdss::Rope rope_view(const mdss_rope* r, int32_t inverse) {
+  mdss::Rope v;
+  v.freq = r->frequencies;
+  v.pairs = r->pairs;
+  v.interleaved = r->interleaved != 0;
+  v.magnitude = r->magnitude;
+  v.sign = inverse ? -1.0f : 1.0f;
+  v.bound = (float)(1.4142135623730951 * (double)r->magnitude);
+  return v;
+}
+
 mdss_status check_beams(int64_t B, int64_t W, int64_t n) {
   if (W < 1 || W > MDSS_MAX_BEAMS || n < 1 || n > MDSS_MAX_BEAMS || B < 0 || B * W > 65535 || B * n > 65535 ||
       B > 65535)
@@ -476,6 +494,108 @@ mdss_status mdss_cache_append(const mdss_cache* cache, int32_t layer, const void
   return from_hip(mdss::launch_cache_append(cache_view(cache), layer, key, value, dtype, key_token_stride,
                                             key_head_stride, value_token_stride, value_head_stride, rows, row_status,
                                             static_cast<hipStream_t>(stream)));
+}
+
+mdss_status mdss_rotary(const void* x, int64_t x_token_stride, int64_t x_head_stride, mdss_dtype dtype, int64_t T, int64_t heads,
+                        int64_t head_dim, const int32_t* positions, const mdss_rope* rope, int32_t inverse, void* out,
+                        int64_t out_token_stride, int64_t out_head_stride, void* stream) {
+  const mdss_status s = check_rope(rope, head_dim);
+  if (s != MDSS_OK) return s;
+  if (T < 0 || T > kMaxTokens || heads < 1 || head_dim > 65536 || heads > INT32_MAX / head_dim) return MDSS_ESHAPE;
+  if (dtype != MDSS_F32 && dtype != MDSS_BF16 && dtype != MDSS_F16) return MDSS_EUNSUPPORTED;
+  if (x_token_stride < 0 || x_head_stride < 0 || (T > 1 && out_token_stride < head_dim) || (heads > 1 && out_head_stride < head_dim))
+    return MDSS_EINVAL;
+  if (T == 0) return MDSS_OK;
+  if (!x || !out || !positions || !rope->frequencies) return MDSS_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) & (dtype == MDSS_F32 ? 3 : 1)) return MDSS_EINVAL;
+  if (x == out && ((T > 1 && x_token_stride != out_token_stride) || (heads > 1 && x_head_stride != out_head_stride))) return MDSS_EINVAL;
+  return from_hip(mdss::launch_rotary(x, x_token_stride, x_head_stride, dtype, T, heads, head_dim, positions, rope_view(rope, inverse), out,
+                                      out_token_stride, out_head_stride, static_cast<hipStream_t>(stream)));
+}
+
+mdss_status mdss_cache_append_rotary(const mdss_cache* cache, int32_t layer, const void* key, int64_t key_token_stride,
+                                     int64_t key_head_stride, const void* value, int64_t value_token_stride,
+                                     int64_t value_head_stride, mdss_dtype dtype, int64_t T, const int32_t* starts,
+                                     const int32_t* table, int64_t width, const int32_t* lengths, int64_t S,
+                                     const mdss_rope* rope, const int32_t* positions, const void* q, int64_t q_token_stride,
+                                     int64_t q_head_stride, int64_t heads_q, void* q_out, int32_t* row_status, void* stream) {
+  mdss_status s = check_cache(cache);
+  if (s != MDSS_OK) return s;
+  if ((s = check_rope(rope, cache->head_dim)) != MDSS_OK) return s;
+  if ((s = check_rows(S, width)) != MDSS_OK) return s;
+  if ((s = check_tokens(T, S, !starts)) != MDSS_OK) return s;
+  if (heads_q < 0 || heads_q % cache->heads || heads_q / cache->heads > 1024 || T * heads_q > INT32_MAX) return MDSS_ESHAPE;
+  if (layer < 0 || layer >= cache->layers || key_token_stride < 0 || key_head_stride < 0 || value_token_stride < 0 ||
+      value_head_stride < 0 || q_token_stride < 0 || q_head_stride < 0)
+    return MDSS_EINVAL;
+  if (dtype != MDSS_BF16 && dtype != MDSS_F16) return MDSS_EUNSUPPORTED;
+  if (S == 0 || T == 0) return MDSS_OK;
+  if (!cache_pointers(cache) || !key || !value || !table || !lengths || !rope->frequencies) return MDSS_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(key) | reinterpret_cast<uintptr_t>(value)) & 1) return MDSS_EINVAL;
+  if (heads_q > 0 && (!q || !q_out || q == q_out || (reinterpret_cast<uintptr_t>(q) & 1) || (reinterpret_cast<uintptr_t>(q_out) & 15)))
+    return MDSS_EINVAL;
+  const mdss::CacheRows rows = {starts, table, lengths, T, width, (int)S};
+  const mdss::AppendTurn turn = {rope_view(rope, 0), positions, q, q_out, q_token_stride, q_head_stride, heads_q * cache->head_dim,
+                                 cache->head_dim, (int)(heads_q / cache->heads)};
+  return from_hip(mdss::launch_cache_append(cache_view(cache), layer, key, value, dtype, key_token_stride, key_head_stride,
+                                            value_token_stride, value_head_stride, rows, row_status,
+                                            static_cast<hipStream_t>(stream), &turn));
+}
+
+mdss_status mdss_cache_shared(const mdss_cache* cache, int64_t T, const int32_t* starts, const int32_t* table, int64_t width,
+                              const int32_t* lengths, int64_t S, const int32_t* groups, int64_t G, int32_t least,
+                              int32_t* tokens, int32_t* group_rows, void* stream) {
+  mdss_status s = check_cache(cache);
+  if (s != MDSS_OK) return s;
+  if ((s = check_rows(S, width)) != MDSS_OK) return s;
+  if ((s = check_tokens(T, S, !starts)) != MDSS_OK) return s;
+  if (G < 0 || G > MDSS_MAX_B) return MDSS_ESHAPE;
+  if (least < 0) return MDSS_EINVAL;
+  if (S == 0 && G == 0) return MDSS_OK;
+  if (G > 0 && (!groups || !group_rows)) return MDSS_EINVAL;
+  if (S > 0 && (!table || !lengths || !tokens)) return MDSS_EINVAL;
+  const mdss::CacheRows rows = {starts, table, lengths, T, width, (int)S};
+  return from_hip(mdss::launch_cache_shared(cache_view(cache), rows, groups, G, least, tokens, group_rows,
+                                            static_cast<hipStream_t>(stream)));
+}
+
+size_t mdss_workspace_bytes_attention_shared(const mdss_cache* cache, int64_t T, int64_t S, int64_t G, int64_t width, int64_t heads_q,
+                                             int32_t uniform, int64_t max_new, int64_t max_group, int64_t max_shared, int64_t max_own) {
+  if (check_cache(cache) != MDSS_OK || check_rows(S, width) != MDSS_OK || check_tokens(T, S, uniform) != MDSS_OK || G < 0 ||
+      G > MDSS_MAX_B || heads_q < 1 || heads_q % cache->heads || heads_q / cache->heads > 1024 || T * heads_q > INT32_MAX || S == 0 ||
+      T == 0)
+    return 0;
+  return mdss::workspace_bytes_attention_shared(cache_view(cache), T, S, G, width, heads_q, uniform != 0, max_new, max_group,
+                                                max_shared, max_own);
+}
+
+mdss_status mdss_cache_attention_shared(const mdss_cache* cache, int32_t layer, const void* q, int64_t q_token_stride,
+                                        int64_t q_head_stride, mdss_dtype dtype, int64_t T, int64_t heads_q,
+                                        const int32_t* starts, const int32_t* table, int64_t width, const int32_t* lengths,
+                                        int64_t S, const int32_t* tokens, const int32_t* group_rows, int64_t G, float scale,
+                                        int64_t max_new, int64_t max_group, int64_t max_shared, int64_t max_own, void* out,
+                                        float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  mdss_status s = check_cache(cache);
+  if (s != MDSS_OK) return s;
+  if ((s = check_rows(S, width)) != MDSS_OK) return s;
+  if ((s = check_tokens(T, S, !starts)) != MDSS_OK) return s;
+  if (G < 0 || G > MDSS_MAX_B || heads_q < 1 || heads_q % cache->heads || heads_q / cache->heads > 1024 || T * heads_q > INT32_MAX)
+    return MDSS_ESHAPE;
+  if (layer < 0 || layer >= cache->layers || q_token_stride < 0 || q_head_stride < 0 || max_new < 0 || max_group < 0 ||
+      max_shared < 0 || max_own < 0)
+    return MDSS_EINVAL;
+  if (dtype != MDSS_BF16 && dtype != MDSS_F16) return MDSS_EUNSUPPORTED;
+  if (S == 0 || T == 0) return MDSS_OK;
+  if (!cache_pointers(cache) || !q || !table || !lengths || !tokens || (G > 0 && !group_rows) || !out) return MDSS_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(q) & 1) || (reinterpret_cast<uintptr_t>(out) & 15)) return MDSS_EINVAL;
+  const mdss::CacheView c = cache_view(cache);
+  const size_t need = mdss::workspace_bytes_attention_shared(c, T, S, G, width, heads_q, !starts, max_new, max_group, max_shared,
+                                                             max_own);
+  if (!workspace_ok(workspace, workspace_bytes, need)) return MDSS_EWORKSPACE;
+  const mdss::CacheRows rows = {starts, table, lengths, T, width, (int)S};
+  return from_hip(mdss::launch_cache_attention_shared(c, layer, q, dtype, heads_q, q_token_stride, q_head_stride, rows, tokens,
+                                                      group_rows, G, scale, max_new, max_group, max_shared, max_own, out, lse,
+                                                      workspace, static_cast<hipStream_t>(stream)));
 }
 
 size_t mdss_workspace_bytes_attention(const mdss_cache* cache, int64_t T, int64_t S, int64_t width, int64_t heads_q,

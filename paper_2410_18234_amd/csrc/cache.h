@@ -9,6 +9,7 @@
 
 #include "common.h"
 #include "mdss.h"
+#include "rotary.h"
 
 namespace mdss {
 
@@ -32,9 +33,21 @@ struct CacheRows {
   int S;
 };
 
+// Keys turned by their positions on the way, and `group` query heads of each cache head turned beside them (0: none).
+struct AppendTurn {
+  Rope rope;
+  const int32_t* positions;
+  const void* q;
+  void* q_out;
+  int64_t q_st, q_sh, qo_st, qo_sh;
+  int group;
+};
+
 hipError_t launch_cache_append(const CacheView& c, int layer, const void* key, const void* value, int dtype,
                                int64_t key_st, int64_t key_sh, int64_t val_st, int64_t val_sh, const CacheRows& rows,
-                               int32_t* row_status, hipStream_t st);
+                               int32_t* row_status, hipStream_t st, const AppendTurn* turn = nullptr);
+hipError_t launch_rotary(const void* x, int64_t x_st, int64_t x_sh, int dtype, int64_t T, int64_t H, int64_t D, const int32_t* positions,
+                         const Rope& rope, void* out, int64_t o_st, int64_t o_sh, hipStream_t st);
 size_t workspace_bytes_cache_fork(int64_t pages, int64_t rows);
 hipError_t launch_cache_fork(const CacheView& c, const int32_t* table, const int32_t* lengths, int64_t S,
                              int64_t width, const int32_t* refs, const int32_t* parent, const int32_t* keep,
@@ -50,6 +63,14 @@ size_t workspace_bytes_attention(const CacheView& c, int64_t T, int64_t S, int64
 hipError_t launch_cache_attention(const CacheView& c, int layer, const void* q, int dtype, int64_t heads_q,
                                   int64_t q_st, int64_t q_sh, const CacheRows& rows, float scale, int64_t max_new,
                                   int64_t max_length, void* out, float* lse, void* workspace, hipStream_t st);
+hipError_t launch_cache_shared(const CacheView& c, const CacheRows& rows, const int32_t* groups, int64_t G, int32_t least,
+                               int32_t* tokens, int32_t* group_rows, hipStream_t st);
+size_t workspace_bytes_attention_shared(const CacheView& c, int64_t T, int64_t S, int64_t G, int64_t width, int64_t heads_q,
+                                        bool uniform, int64_t max_new, int64_t max_group, int64_t max_shared, int64_t max_own);
+hipError_t launch_cache_attention_shared(const CacheView& c, int layer, const void* q, int dtype, int64_t heads_q, int64_t q_st,
+                                         int64_t q_sh, const CacheRows& rows, const int32_t* tokens, const int32_t* groups, int64_t G,
+                                         float scale, int64_t max_new, int64_t max_group, int64_t max_shared, int64_t max_own,
+                                         void* out, float* lse, void* workspace, hipStream_t st);
 size_t workspace_bytes_beam(int64_t B, int64_t W, int64_t V, int64_t n);
 hipError_t launch_beam_select(const void* logits, int dtype, int64_t row_stride, const float* scores,
                               const uint8_t* done, int64_t B, int64_t W, int64_t V, int64_t n, int32_t eos,
@@ -66,14 +87,14 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Sequence of the slot `slot`, where sequence s owns the slots from first(s) = floor(starts[s] * num / den) + extra
 // * s on: the largest s with first(s) <= slot (first is monotone in s).  The wave reads 64 candidates a step, so
-// 4096 sequences take two dependent loads.
+// 4096 sequences take two dependent loads.  (Their starts lie `stride` apart.)
 __device__ __forceinline__ int slot_sequence(const int32_t* starts, int S, int64_t slot, int num, int den, int extra,
-                                             int lane) {
+                                             int lane, int stride = 1) {
   int lo = 0, n = S;  // the answer is in [lo, lo + n)
   while (n > 1) {
     const int step = (n + 63) >> 6;
     const int s = lo + lane * step;
-    const bool le = s < lo + n && (int64_t)starts[s] * num / den + (int64_t)extra * s <= slot;
+    const bool le = s < lo + n && (int64_t)starts[(int64_t)s * stride] * num / den + (int64_t)extra * s <= slot;
     const int hits = __popcll(__ballot(le));  // lane 0 always hits
     const int at = hits > 0 ? hits - 1 : 0;
     lo += at * step;
@@ -81,8 +102,8 @@ __device__ __forceinline__ int slot_sequence(const int32_t* starts, int S, int64
   }
   return lo;
 }
-__device__ __forceinline__ int64_t slot_first(const int32_t* starts, int s, int num, int den, int extra) {
-  return (int64_t)starts[s] * num / den + (int64_t)extra * s;
+__device__ __forceinline__ int64_t slot_first(const int32_t* starts, int s, int num, int den, int extra, int stride = 1) {
+  return (int64_t)starts[(int64_t)s * stride] * num / den + (int64_t)extra * s;
 }
 
 }  // namespace mdss

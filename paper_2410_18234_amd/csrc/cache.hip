@@ -3,6 +3,7 @@
 //
 // Page ids come from the caller's tables: an id outside [0, pages) is never followed.
 #include "cache.h"
+#include "rotary.h"
 
 namespace mdss {
 
@@ -65,14 +66,121 @@ struct AppendArgs {
   int heads, page_shift, per_seq;
   bool key_al, val_al;
   int32_t* row_status;
+  // keys turned by their positions on the way, and queries beside them
+  Rope rope;
+  const int32_t* positions;  // of each new token (null: its place in its sequence)
+  const uint16_t* q;
+  uint16_t* q_out;
+  int64_t q_st, q_sh, qo_st, qo_sh;
+  int group;  // query heads of a cache head (0: no queries)
+  bool q_al;
+  bool halves;  // pairs lie half of the turned part apart, in whole pieces of 8
 };
+
+// Two pieces of 8 elements of a token, which a thread turns together: those at the same place of both halves of the turned part, or
+// neighbours (pairs side by side, halves that are not whole pieces, and what is not turned).
+struct Bundle {
+  int first, second;  // pieces of the token
+  bool pairs;         // they are each other's pairs
+};
+__device__ __forceinline__ Bundle bundle_of(const AppendArgs& a, int b) {
+  const int half = a.halves ? a.rope.pairs >> 3 : 0;
+  if (b < half) return {b, b + half, true};
+  return {2 * b, 2 * b + 1, false};  // (2 half + 2 (b - half))
+}
+
+// The bundle's elements times `scale` (a power of two, before anything that could pass fp32's range) at `position`, turned, in fp32.
+// at: the token's elements.
+template <bool BF>
+__device__ __forceinline__ void turn_bundle(const AppendArgs& a, const Bundle& b, double position, float scale, const uint16_t* at,
+                                            const u32x4& first, const u32x4& second, float (&x)[8], float (&y)[8]) {
+  using P = Pack<BF ? 1 : 2>;
+  P::open(first, x);
+  P::open(second, y);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[i] *= scale;
+    y[i] *= scale;
+  }
+  const int pairs = a.rope.pairs;
+  if (b.pairs) {
+    const double* f = a.rope.freq + 8 * b.first;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float c, s;
+      turn(a.rope, position, f[i], c, s);
+      const float u = x[i], v = y[i];
+      x[i] = turned_first(u, v, c, s);
+      y[i] = turned_second(u, v, c, s);
+    }
+    return;
+  }
+  const auto piece = [&](float (&z)[8], int d0) __attribute__((always_inline)) {
+    if (d0 >= 2 * pairs) return;
+    if (a.rope.interleaved) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 2)
+        if (d0 + i < 2 * pairs) {
+          float c, s;
+          turn(a.rope, position, a.rope.freq[(d0 + i) >> 1], c, s);
+          const float u = z[i], v = z[i + 1];
+          z[i] = turned_first(u, v, c, s);
+          z[i + 1] = turned_second(u, v, c, s);
+        }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < 8; ++i) {
+        const int d = d0 + i;
+        if (d >= 2 * pairs) break;
+        float c, s;
+        const bool up = d >= pairs;
+        turn(a.rope, position, a.rope.freq[up ? d - pairs : d], c, s);
+        const float mine = P::widen(__builtin_bit_cast(typename P::one, at[d])) * scale,
+                    other = P::widen(__builtin_bit_cast(typename P::one, at[up ? d - pairs : d + pairs])) * scale;
+        const float to = up ? turned_second(other, mine, c, s) : turned_first(mine, other, c, s);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = j == i ? to : z[j];
+      }
+    }
+  };
+  piece(x, 8 * b.first);
+  piece(y, 8 * b.second);
+}
+
+// The queries of `cnt` tokens from `tok` on (in their sequence from `pos` on), of the query heads of cache head h.
+template <int D, bool BF, int NT>
+__device__ __forceinline__ void turn_queries(const AppendArgs& a, int h, int64_t tok, int64_t pos, int cnt) {
+  constexpr int kBundles = D / 16;
+  const int total = cnt * kBundles;
+  // threads that a bundle's heads are divided between
+  const int slices = total >= NT ? 1 : min(a.group, NT / total);
+  for (int e = threadIdx.x; e < total * slices; e += NT) {
+    const int slice = e / total, rest = e - slice * total, i = rest / kBundles;
+    const Bundle b = bundle_of(a, rest - i * kBundles);
+    const double position = a.positions ? (double)a.positions[tok + i] : (double)(pos + i);
+    for (int j = slice; j < a.group; j += slices) {
+      const int64_t head = (int64_t)h * a.group + j;
+      const uint16_t* at = a.q + (tok + i) * a.q_st + head * a.q_sh;
+      float x[8], y[8];
+      turn_bundle<BF>(a, b, position, 1.0f, at, load8(at + 8 * b.first, a.q_al), load8(at + 8 * b.second, a.q_al), x, y);
+      uint16_t* to = a.q_out + (tok + i) * a.qo_st + head * a.qo_sh;
+      const u32x4 first = Pack<BF ? 1 : 2>::close(x), second = Pack<BF ? 1 : 2>::close(y);
+      *reinterpret_cast<u32x4*>(to + 8 * b.first) = first;
+      *reinterpret_cast<u32x4*>(to + 8 * b.second) = second;
+    }
+  }
+}
 
 // A workgroup of NT threads writes the new tokens of one page and head, keys and values.  They are read once (kHeld pieces of
 // 8 a thread of each stay in registers between the maximum and the rounding; longer pages are read again), keys and
 // values together, since what a workgroup waits for is the chain starts - lengths - table - tokens.  Values go
 // through LDS to become 16 tokens a row of d.  Bound by memory on prompts (16 x up to 2048 tokens, 8 heads of 128, 174 MB: 44 us,
 // 3.9 TB/s), by the launch on single tokens (256 of them: 12 us a call).
-template <int D, bool BF, int NT>
+//
+// TURN: keys are turned by their positions in fp32 and rounded once.  The exponent is that of a bound, sqrt(2) m times the largest
+// magnitude of the turned part, which no angle passes: it is known before the angles are, and does not hang on their rounding.  (A power
+// of two costs a code nothing but its smallest values.)  Workgroups with y from `heads` on turn the queries of the same tokens.
+template <int D, bool BF, int NT, bool TURN>
 __global__ __launch_bounds__(NT, 4) void append_kernel(const AppendArgs a) {
   constexpr int kHeld = NT == 64 ? 2 : 4;
   constexpr int kLine = D / 8;           // pieces of a token
@@ -80,7 +188,8 @@ __global__ __launch_bounds__(NT, 4) void append_kernel(const AppendArgs a) {
   __shared__ __align__(16) uint8_t slab[kSlab * (D + 4)];
   __shared__ float red[2][NT / 64];
   const int tid = threadIdx.x, lane = tid & 63;
-  const int h = blockIdx.y, ps = 1 << a.page_shift;
+  const int ps = 1 << a.page_shift;
+  int h = blockIdx.y;
   const int64_t slot = blockIdx.x;
   int s, i;
   if (a.per_seq > 0) {
@@ -101,6 +210,14 @@ __global__ __launch_bounds__(NT, 4) void append_kernel(const AppendArgs a) {
   }
   if (start < 0 || n <= 0 || start + n > a.rows.T) return;
   const int len = a.rows.lengths[s], before = len - n;
+  if constexpr (TURN) {
+    if (h >= a.heads) {  // (tokens without a page have queries all the same)
+      const int64_t from = (int64_t)len - n, base = ((from >> a.page_shift) + i) << a.page_shift;
+      const int64_t o = max(from, base), to = min((int64_t)len, base + ps);
+      if (i >= 0 && o < to) turn_queries<D, BF, NT>(a, h - a.heads, start + (o - from), o, (int)(to - o));
+      return;
+    }
+  }
   const bool fits = before >= 0 && (int64_t)len <= a.rows.width << a.page_shift;
   if (!fits) {
     if (i == 0 && h == 0 && tid == 0 && a.row_status) atomicOr(a.row_status + s, kRowNoPage);
@@ -121,16 +238,24 @@ __global__ __launch_bounds__(NT, 4) void append_kernel(const AppendArgs a) {
   const int64_t ph = (int64_t)page * a.heads + h;
   uint8_t *kd = a.k + (ph << a.page_shift) * D, *vd = a.v + (ph << a.page_shift) * D;
   const auto fetch_k = [&](int e) { return load8(kx + (int64_t)(e / kLine) * a.key_st + (e % kLine) * 8, a.key_al); };
+  // key pieces in the order that a thread holds them: TURN: bundles, two pieces each
+  const auto key_piece = [&](int j, int e) {
+    if (!TURN) return e;
+    const int t = e / (kLine / 2);
+    const Bundle b = bundle_of(a, e - t * (kLine / 2));
+    return t * kLine + (j & 1 ? b.second : b.first);
+  };
+  const auto key_place = [&](int j) { return TURN ? tid + NT * (j >> 1) : tid + NT * j; };
+  const int key_total = TURN ? total / 2 : total;
   const auto fetch_v = [&](int e) { return load8(vx + (int64_t)(e / kLine) * a.val_st + (e % kLine) * 8, a.val_al); };
 
   // the largest magnitudes
   u32x4 kh[kHeld], vh[kHeld];
 #pragma unroll
-  for (int j = 0; j < kHeld; ++j)
-    if (tid + NT * j < total) {
-      kh[j] = fetch_k(tid + NT * j);
-      vh[j] = fetch_v(tid + NT * j);
-    }
+  for (int j = 0; j < kHeld; ++j) {
+    if (key_place(j) < key_total) kh[j] = fetch_k(key_piece(j, key_place(j)));
+    if (tid + NT * j < total) vh[j] = fetch_v(tid + NT * j);
+  }
   int ke = kCacheMinExp, ve = kCacheMinExp;  // of the page's earlier tokens
   if (o > 0) {
     ke = a.k_exp[ph];
@@ -142,17 +267,33 @@ __global__ __launch_bounds__(NT, 4) void append_kernel(const AppendArgs a) {
       m = fmaxf(m, fmaxf(finite_abs(widen16<BF>((uint16_t)r[w])), finite_abs(widen16<BF>((uint16_t)(r[w] >> 16)))));
     return m;
   };
+  // (TURN: by the bound)
+  const auto largest_key = [&](u32x4 r, int e, float m) {
+    if (!TURN) return largest(r, m);
+    const int d0 = e % kLine * 8, dim = 2 * a.rope.pairs;
+    if (d0 >= dim) return largest(r, m);
+    if (d0 + 8 <= dim) return fmaxf(m, fminf(largest(r, 0.0f) * a.rope.bound, 3.4028235e38f));
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {  // (dim is even)
+      const float two = fmaxf(finite_abs(widen16<BF>((uint16_t)r[w])), finite_abs(widen16<BF>((uint16_t)(r[w] >> 16))));
+      m = fmaxf(m, d0 + 2 * w < dim ? fminf(two * a.rope.bound, 3.4028235e38f) : two);
+    }
+    return m;
+  };
   float km = 0.0f, vm = 0.0f;
 #pragma unroll
-  for (int j = 0; j < kHeld; ++j)
-    if (tid + NT * j < total) {
-      km = largest(kh[j], km);
-      vm = largest(vh[j], vm);
-    }
+  for (int j = 0; j < kHeld; ++j) {
+    if (key_place(j) < key_total) km = largest_key(kh[j], key_piece(j, key_place(j)), km);
+    if (tid + NT * j < total) vm = largest(vh[j], vm);
+  }
   for (int e = tid + NT * kHeld; e < total; e += NT) {
-    km = largest(fetch_k(e), km);
+    if (!TURN) km = largest(fetch_k(e), km);
     vm = largest(fetch_v(e), vm);
   }
+  if (TURN)
+    for (int e = key_place(kHeld); e < key_total; e += NT)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) km = largest_key(fetch_k(key_piece(j, e)), key_piece(j, e), km);
   km = wave_max(km);
   vm = wave_max(vm);
   if (NT > 64) {
@@ -210,14 +351,36 @@ __global__ __launch_bounds__(NT, 4) void append_kernel(const AppendArgs a) {
     return c;
   };
   const float kf = pow2f(-ke_new), vf = pow2f(-ve_new);
-  const auto put_k = [&](int e, u32x4 r) {
+  const auto key_spot = [&](int e) {
     const int t = o + e / kLine, d8 = e % kLine;
-    *reinterpret_cast<u32x2*>(kd + (t >> 4) * (16 * D) + (d8 >> 1) * 256 + (t & 15) * 16 + (d8 & 1) * 8) = encode(r, kf);
+    return reinterpret_cast<u32x2*>(kd + (t >> 4) * (16 * D) + (d8 >> 1) * 256 + (t & 15) * 16 + (d8 & 1) * 8);
   };
+  if constexpr (TURN) {
+    const auto put_bundle = [&](int e, const u32x4& first, const u32x4& second) __attribute__((always_inline)) {
+      const int i = e / (kLine / 2);
+      const Bundle b = bundle_of(a, e - i * (kLine / 2));
+      const double position = a.positions ? (double)a.positions[tok + i] : (double)(base + o + i);
+      float x[8], y[8];
+      turn_bundle<BF>(a, b, position, kf, kx + (int64_t)i * a.key_st, first, second, x, y);
+      u32x2 cx, cy;
 #pragma unroll
-  for (int j = 0; j < kHeld; ++j)
-    if (tid + NT * j < total) put_k(tid + NT * j, kh[j]);
-  for (int e = tid + NT * kHeld; e < total; e += NT) put_k(e, fetch_k(e));
+      for (int w = 0; w < 2; ++w) {
+        cx[w] = codes_of(x[4 * w], x[4 * w + 1]) | codes_of(x[4 * w + 2], x[4 * w + 3]) << 16;
+        cy[w] = codes_of(y[4 * w], y[4 * w + 1]) | codes_of(y[4 * w + 2], y[4 * w + 3]) << 16;
+      }
+      *key_spot(i * kLine + b.first) = cx;
+      *key_spot(i * kLine + b.second) = cy;
+    };
+#pragma unroll
+    for (int j = 0; j < kHeld; j += 2)
+      if (key_place(j) < key_total) put_bundle(key_place(j), kh[j], kh[j + 1]);
+    for (int e = key_place(kHeld); e < key_total; e += NT) put_bundle(e, fetch_k(key_piece(0, e)), fetch_k(key_piece(1, e)));
+  } else {
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+      if (tid + NT * j < total) *key_spot(tid + NT * j) = encode(kh[j], kf);
+    for (int e = tid + NT * kHeld; e < total; e += NT) *key_spot(e) = encode(fetch_k(e), kf);
+  }
   // values: kSlab tokens (from a unit's start) at a time through LDS, [token][D + 4]
   const int last = o + cnt;
   for (int c0 = o & ~15; c0 < last; c0 += kSlab) {
@@ -259,12 +422,19 @@ __global__ __launch_bounds__(NT, 4) void append_kernel(const AppendArgs a) {
   }
 }
 
+template <int D, bool BF, bool TURN>
+void append_launch_turned(const AppendArgs& a, dim3 grid, bool small, hipStream_t st) {
+  if (small)
+    append_kernel<D, BF, 64, TURN><<<grid, 64, 0, st>>>(a);
+  else
+    append_kernel<D, BF, 256, TURN><<<grid, 256, 0, st>>>(a);
+}
 template <int D, bool BF>
 void append_launch(const AppendArgs& a, dim3 grid, bool small, hipStream_t st) {
-  if (small)
-    append_kernel<D, BF, 64><<<grid, 64, 0, st>>>(a);
+  if (a.rope.freq)
+    append_launch_turned<D, BF, true>(a, grid, small, st);
   else
-    append_kernel<D, BF, 256><<<grid, 256, 0, st>>>(a);
+    append_launch_turned<D, BF, false>(a, grid, small, st);
 }
 
 // ---------------------------------------------------------------- fork and compact: shared pieces
@@ -856,8 +1026,8 @@ __global__ __launch_bounds__(kThreads) void compact_move_kernel(CompactArgs a) {
 
 hipError_t launch_cache_append(const CacheView& c, int layer, const void* key, const void* value, int dtype,
                                int64_t key_st, int64_t key_sh, int64_t val_st, int64_t val_sh, const CacheRows& rows,
-                               int32_t* row_status, hipStream_t st) {
-  AppendArgs a;
+                               int32_t* row_status, hipStream_t st, const AppendTurn* turn) {
+  AppendArgs a = {};
   a.rows = rows;
   a.key = static_cast<const uint16_t*>(key);
   a.val = static_cast<const uint16_t*>(value);
@@ -879,7 +1049,20 @@ hipError_t launch_cache_append(const CacheView& c, int layer, const void* key, c
   const int64_t n = rows.T / rows.S;
   a.per_seq = rows.starts ? 0 : n == 1 ? 1 : (int)(((n - 1) >> c.page_shift) + 2);
   const int64_t slots = rows.starts ? (rows.T >> c.page_shift) + 2 * (int64_t)rows.S : (int64_t)rows.S * a.per_seq;
-  const dim3 grid((unsigned)slots, (unsigned)c.heads);
+  if (turn) {
+    a.rope = turn->rope;
+    a.positions = turn->positions;
+    a.halves = !a.rope.interleaved && a.rope.pairs % 8 == 0;
+    a.q = static_cast<const uint16_t*>(turn->q);
+    a.q_out = static_cast<uint16_t*>(turn->q_out);
+    a.q_st = turn->q_st;
+    a.q_sh = turn->q_sh;
+    a.qo_st = turn->qo_st;
+    a.qo_sh = turn->qo_sh;
+    a.group = turn->group;
+    a.q_al = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && a.q_st % 8 == 0 && a.q_sh % 8 == 0;
+  }
+  const dim3 grid((unsigned)slots, (unsigned)(a.group > 0 ? 2 * c.heads : c.heads));
   // few tokens a page: a wave is enough
   const bool small = rows.T <= 2 * (int64_t)rows.S, bf = dtype == MDSS_BF16;
   switch (c.d) {
