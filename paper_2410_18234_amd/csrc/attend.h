@@ -53,8 +53,8 @@ struct AttendArgs {
   bool negative;
   // calls with shared prefixes: workgroups of the prefixes first, then (from pre_blocks on) those of the sequences' own tokens
   const int32_t *tokens, *groups;  // tokens [S]: those a sequence reads with its group; groups [G][4]: first new token, new tokens, row, tokens
-  int64_t block0, pre_blocks;
-  int G, pre_slots, slots, pre_splits, pre_split_tiles;
+  int64_t block0, pre_blocks;      // (blocks: of workgroups, or where own_waves is 1, of waves past pre_blocks)
+  int G, pre_slots, slots, pre_splits, pre_split_tiles, own_waves;
 };
 
 template <bool BF>
@@ -180,10 +180,23 @@ __device__ __forceinline__ int shared_tokens(const AttendArgs& a, int s, int bef
   return t > 0 && t <= before ? t & ~63 : 0;
 }
 
+// The set (a sequence, or a group) and the row tile of a slot, where set i's rows begin with token starts[i * stride]: the sets' first tiles, then
+// the others.  (Slots without rows lie at the end so: among the others they leave every second one empty where sets fill half of
+// their tiles, and with them half of the shader engines, which workgroups go round in order: 64 groups of 32 rows over 6000 tokens took 258 us.)
+__device__ __forceinline__ void slot_tile(const int32_t* starts, int sets, int slot, int group, int tile_rows, int lane, int stride, int& set,
+                                          int& tile) {
+  set = slot;
+  tile = 0;
+  if (slot >= sets) {
+    set = slot_sequence(starts, sets, slot - sets, group, tile_rows, 0, lane, stride);
+    tile = 1 + slot - sets - (int)slot_first(starts, set, group, tile_rows, 0, stride);
+  }
+}
+
 // A workgroup over a group's shared tokens: the new tokens of all its sequences are the rows, and all of them see all of it.
 __device__ __forceinline__ bool prefix_place(const AttendArgs& a, int slot, int tile_rows, int lane, Place& p) {
-  const int g = slot_sequence(a.groups, a.G, slot, a.group, tile_rows, 1, lane, 4);
-  p.tile = slot - (int)slot_first(a.groups, g, a.group, tile_rows, 1, 4);
+  int g;
+  slot_tile(a.groups, a.G, slot, a.group, tile_rows, lane, 4, g, p.tile);
   const i32x4 row = *reinterpret_cast<const i32x4*>(a.groups + 4 * (int64_t)g);
   p.start = row[0];
   p.n = row[1];
@@ -198,17 +211,18 @@ __device__ __forceinline__ bool prefix_place(const AttendArgs& a, int slot, int 
 // The head is the fastest index of the grid: the row tiles that read one head's pages run on the same XCD where heads
 // are a multiple of 8 (workgroups go round the XCDs in order), and find them in its L2.  A sequence's last rows, which see the
 // most tokens, start first (a prompt of 3000 tokens, 64 query heads: 205 us, 246 the other way round).
+// (SHARED: `block` is the workgroup's, or a wave's, among the launches' together.)
 template <bool SHARED>
-__device__ __forceinline__ bool attend_place(const AttendArgs& a, int tile_rows, int lane, Place& p) {
+__device__ __forceinline__ bool attend_place(const AttendArgs& a, int tile_rows, int lane, Place& p, int64_t block = 0) {
   int slot;
   p.first = 0;
   if constexpr (SHARED) {
-    const int64_t block = a.block0 + blockIdx.x;
     const bool prefix = block < a.pre_blocks;
     const uint32_t b = (uint32_t)(prefix ? block : block - a.pre_blocks), slots = prefix ? a.pre_slots : a.slots;
     const uint32_t part = b / (uint32_t)a.heads;
     p.h = b - part * a.heads;
     p.split = part / slots;
+    if (!prefix && p.split >= a.splits) return false;  // (the last workgroup's waves past the end)
     slot = part - p.split * slots;
     p.splits = prefix ? a.pre_splits : a.splits;
     p.split_tiles = prefix ? a.pre_split_tiles : a.split_tiles;
@@ -228,6 +242,8 @@ __device__ __forceinline__ bool attend_place(const AttendArgs& a, int tile_rows,
   if (a.per_seq > 0) {
     p.s = slot / a.per_seq;
     p.tile = slot - p.s * a.per_seq;
+  } else if constexpr (SHARED) {
+    slot_tile(a.starts, a.S, slot, a.group, tile_rows, lane, 1, p.s, p.tile);
   } else {
     p.s = slot_sequence(a.starts, a.S, slot, a.group, tile_rows, 1, lane);
     p.tile = slot - (int)slot_first(a.starts, p.s, a.group, tile_rows, 1);
@@ -371,11 +387,17 @@ __device__ __forceinline__ void weigh(const f32x4 (&sc)[4][MT], float c_g, float
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float p = __builtin_amdgcn_exp2f(fmaf(sc[tt][r][i], c_g, off));
-        if (MASKED) p = 4 * tt + i < upto[r] ? p : 0.0f;
-        sum += p;
-        pf[r][tt >> 1][4 * (tt & 1) + i] = (_Float16)p;
+      for (int i = 0; i < 4; i += 2) {
+        f32x2 p;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          p[j] = __builtin_amdgcn_exp2f(fmaf(sc[tt][r][i + j], c_g, off));
+          if (MASKED) p[j] = 4 * tt + i + j < upto[r] ? p[j] : 0.0f;
+          sum += p[j];
+        }
+        const f16x2 h = __builtin_convertvector(p, f16x2);  // (one instruction for both)
+        pf[r][tt >> 1][4 * (tt & 1) + i] = h[0];
+        pf[r][tt >> 1][4 * (tt & 1) + i + 1] = h[1];
       }
     l[r] = fmaf(sum, inv_v, l[r]);
 #pragma unroll
@@ -493,6 +515,42 @@ __device__ __forceinline__ void mark_nan(const u32x4& v, const int (&upto)[MT], 
   }
 }
 
+// What a wave has of its rows: the result, or their part of it.
+template <int D, bool BF, int MT>
+__device__ __forceinline__ void write_rows(const AttendArgs& a, const Place& p, int row0, int m, int g, const f32x4 (&acc)[D / 16][MT],
+                                           const float (&M)[MT], const float (&l)[MT]) {
+  typedef typename Elem<BF>::one one;
+  const int64_t heads_q = (int64_t)a.heads * a.group;
+#pragma unroll
+  for (int r = 0; r < MT; ++r) {
+    const int row = row0 + 16 * r + m;
+    if (row >= p.rows) continue;
+    const int i = row / a.group;
+    const int64_t id = (p.start + i) * heads_q + p.h * a.group + (row - i * a.group);
+    if (p.whole) {
+      const float inv = l[r] == 0.0f ? 0.0f : 1.0f / l[r];
+      one* o = static_cast<one*>(a.out) + id * D + 4 * g;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) {
+        typedef one one4 __attribute__((ext_vector_type(4)));
+        one4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (one)(l[r] == 0.0f ? 0.0f : acc[dt][r][e] * inv);
+        *reinterpret_cast<one4*>(o + 16 * dt) = w;
+      }
+      if (a.lse && g == 0) a.lse[id] = log_sum(M[r], l[r]);
+    } else {
+      float* o = a.part + (id * p.parts + p.part) * D + 4 * g;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4*>(o + 16 * dt) = acc[dt][r];
+      if (g == 0) {
+        a.part_ml[2 * (id * p.parts + p.part)] = M[r];
+        a.part_ml[2 * (id * p.parts + p.part) + 1] = l[r];
+      }
+    }
+  }
+}
+
 template <int MT>
 __device__ __forceinline__ void add_values(const f16x8 (&v)[2], const f16x8 (&pf)[MT][2], f32x4 (&acc)[MT]) {
 #pragma unroll
@@ -505,8 +563,9 @@ __device__ __forceinline__ void add_values(const f16x8 (&v)[2], const f16x8 (&pf
 // to registers, and join at the end.  Bound by memory: a tile's keys are loaded while the one before is
 // weighed, its values while its keys are multiplied.  4 x 131072 tokens, 8 heads of 128: 194 us, 5.5 TB/s; 64 sequences of 1024 to
 // 4096 tokens with up to 5 new ones: 66 us, 4.3 TB/s.
+// NW = 1: a wave has rows of its own, and writes what it has by itself.
 constexpr int joined_part(int D) { return 16 * (D + 4); }  // floats of a wave
-template <int D, bool BF, int MT>
+template <int D, bool BF, int MT, int NW = 4>
 __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p, float* joined, float* joined_ml,
                                             typename Elem<BF>::vec* queries) {
   using E = Elem<BF>;
@@ -517,10 +576,9 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
   constexpr bool kHalf = D % 64 != 0;  // and one of 8 bytes
   constexpr int kTiles = D / 16;       // accumulator tiles over d
   constexpr int kPad = D + 4;
-  constexpr int NW = 4;  // waves
 
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row0 = p.tile * 16 * MT, h = p.h;
   const int lim_lo = seen_by(a, p, row0), lim_hi = seen_by(a, p, row0 + 16 * MT - 1);
   const int tiles = lim_hi > 0 ? (lim_hi + 63) >> 6 : 0;
@@ -538,7 +596,7 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
 #pragma unroll
         for (int st = 0; st < kSteps; ++st) queries[(r * kSteps + st) * 64 + lane] = qf[r][st];
     }
-    __syncthreads();
+    if (NW > 1) __syncthreads();  // (a lane reads what it wrote itself)
   }
   f32x4 acc[kTiles][MT];
   float M[MT], l[MT];
@@ -692,9 +750,13 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
   pass(Flag<false>{});
   if (t0 < t_end && lacks<MT, kTiles>(acc, M, lim, least, ve_least, ve_most, 64.0f * ((t_end - t0 + NW - 1) / NW))) pass(Flag<true>{});
 
-  // join the four waves, 16 rows at a time: thread -> a row and a share of its elements
 #pragma unroll
   for (int r = 0; r < MT; ++r) l[r] = row_sum4(l[r]);
+  if constexpr (NW == 1) {
+    write_rows<D, BF, MT>(a, p, row0, m, g, acc, M, l);
+    return;
+  }
+  // join the four waves, 16 rows at a time: thread -> a row and a share of its elements
   const int64_t heads_q = (int64_t)a.heads * a.group;
   constexpr int kShare = D / (4 * NW);  // elements of a thread
   const int jr = threadIdx.x / (4 * NW), jd = threadIdx.x % (4 * NW) * kShare;
@@ -754,13 +816,13 @@ __device__ __forceinline__ void attend_rows(const AttendArgs& a, const Place& p,
 // A sequence that fills fewer of the row tiles than the batch's most multiplies as many as it fills (64 sequences of 2000 tokens with
 // up to 6 new ones, 8 query heads a cache head: 64 us, 77 with all tiles; 64 x up to 4096 with up to 5: 66 and 71).
 // (The bounds are the workgroups a CU that attend_plan counts on: what does not fit the registers then is the precise pass's.)
-template <int D, bool BF, int MT, bool SHARED = false>
+template <int D, bool BF, int MT>
 __global__ __launch_bounds__(256, D > 128 || MT > 2 ? 1 : MT == 2 || D > 96 ? 2 : D == 96 ? 3 : 4) void attend_kernel(const AttendArgs a) {
   __shared__ __align__(16) float joined[4 * joined_part(D)];
   __shared__ float joined_ml[4 * 16 * 2];
   __shared__ __align__(16) typename Elem<BF>::vec queries[MT * D / 32 * 64];  // the same for all four waves: LDS spares their registers
   Place p;
-  if (!attend_place<SHARED>(a, 16 * MT, threadIdx.x & 63, p)) return;
+  if (!attend_place<false>(a, 16 * MT, threadIdx.x & 63, p)) return;
   if (MT > 1 && p.rows <= 16)
     attend_rows<D, BF, 1>(a, p, joined, joined_ml, queries);
   else if (MT > 2 && p.rows <= 32)
@@ -779,7 +841,6 @@ template <int D, bool BF, int MT, bool SHARED = false>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const AttendArgs a) {
   using E = Elem<BF>;
   using vec = typename E::vec;
-  using one = typename E::one;
   constexpr int kSteps = D / 32, kWhole = D / 64, kTiles = D / 16;
   constexpr bool kHalf = D % 64 != 0;
   constexpr int kKeys = 4 * kWhole, kGroups = kKeys + kTiles;  // a lane's 16 codes: of keys (tt, i), then of values (dt)
@@ -794,7 +855,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Place p;
-  if (!attend_place<SHARED>(a, 64 * MT, lane, p)) return;
+  if (!attend_place<SHARED>(a, 64 * MT, lane, p, a.block0 + blockIdx.x)) return;
   const int tile0 = p.tile * 64 * MT, row0 = tile0 + wave * 16 * MT, h = p.h;
   const int lim_first = seen_by(a, p, tile0), lim_lo = seen_by(a, p, row0), lim_wave = row0 < p.rows ? seen_by(a, p, row0 + 16 * MT - 1) : 0;
   const int lim_hi = seen_by(a, p, tile0 + 64 * MT - 1);
@@ -992,44 +1053,17 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_wide_kernel(const
   __syncthreads();
   if (again_any[0] | again_any[1] | again_any[2] | again_any[3]) pass(Flag<true>{}, again);
 
-  const int64_t heads_q = (int64_t)a.heads * a.group;
 #pragma unroll
-  for (int r = 0; r < MT; ++r) {
-    const float ls = row_sum4(l[r]);
-    const int row = row0 + 16 * r + m;
-    if (row >= p.rows) continue;
-    const int i = row / a.group;
-    const int64_t id = (p.start + i) * heads_q + h * a.group + (row - i * a.group);
-    if (p.whole) {
-      const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
-      one* o = static_cast<one*>(a.out) + id * D + 4 * g;
-#pragma unroll
-      for (int dt = 0; dt < kTiles; ++dt) {
-        typedef one one4 __attribute__((ext_vector_type(4)));
-        one4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = (one)(ls == 0.0f ? 0.0f : acc[dt][r][e] * inv);
-        *reinterpret_cast<one4*>(o + 16 * dt) = w;
-      }
-      if (a.lse && g == 0) a.lse[id] = log_sum(M[r], ls);
-    } else {
-      float* o = a.part + (id * p.parts + p.part) * D + 4 * g;
-#pragma unroll
-      for (int dt = 0; dt < kTiles; ++dt) *reinterpret_cast<f32x4*>(o + 16 * dt) = acc[dt][r];
-      if (g == 0) {
-        a.part_ml[2 * (id * p.parts + p.part)] = M[r];
-        a.part_ml[2 * (id * p.parts + p.part) + 1] = ls;
-      }
-    }
-  }
+  for (int r = 0; r < MT; ++r) l[r] = row_sum4(l[r]);
+  write_rows<D, BF, MT>(a, p, row0, m, g, acc, M, l);
 }
 
-// Joins the parts of a row (the splits of the sequence's own tokens; before them, SHARED, those of the tokens it shares): one wave a row.
-template <int D, bool BF, bool SHARED = false>
-__global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, int rows_tile, int64_t total, int64_t first_row) {
+// Joins the splits of a row: one wave a row.
+template <int D, bool BF>
+__global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, int rows_tile, int64_t total) {
   using one = typename Elem<BF>::one;
   const int lane = threadIdx.x & 63;
-  const int64_t id = first_row + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (id >= total) return;
   const int heads_q = a.heads * a.group;
   const int64_t t = id / heads_q;
@@ -1052,22 +1086,14 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, in
   const int len = max(0, min(a.lengths[s], (int)min(a.width << a.page_shift, (int64_t)INT32_MAX)));
   const int before = a.lengths[s] - n;
   const int lim_hi = min(len, before + min(rows - 1, row0 + rows_tile - 1) / a.group + 1);
-  int tiles = lim_hi > 0 ? (lim_hi + 63) >> 6 : 0;
-  // the parts that had tokens for the row's tile
-  int prefix = 0, stride = a.splits, skip = 0;
-  if constexpr (SHARED) {
-    const int first = shared_tokens(a, s, before) >> 6;
-    prefix = min(a.pre_splits, (first + a.pre_split_tiles - 1) / a.pre_split_tiles);
-    stride = a.pre_splits + a.splits;
-    skip = a.pre_splits - prefix;
-    tiles -= first;
-  }
-  const int parts = prefix + max(1, min(a.splits, (tiles + a.split_tiles - 1) / a.split_tiles));
-  const auto part_at = [&](int i) { return id * stride + (SHARED && i >= prefix ? i + skip : i); };
+  const int tiles = lim_hi > 0 ? (lim_hi + 63) >> 6 : 0;
+  // the splits that had tokens for the row's tile
+  const int splits = max(1, min(a.splits, (tiles + a.split_tiles - 1) / a.split_tiles));
+  const float* ml = a.part_ml + 2 * id * a.splits;
   float M = -INFINITY, l = 0.0f;
-  for (int i = lane; i < parts; i += 64) M = fmaxf(M, a.part_ml[2 * part_at(i)]);
+  for (int i = lane; i < splits; i += 64) M = fmaxf(M, ml[2 * i]);
   const float top = wave_max(M);
-  for (int i = lane; i < parts; i += 64) l = fmaf(frame_weight(a.part_ml[2 * part_at(i)], top), a.part_ml[2 * part_at(i) + 1], l);
+  for (int i = lane; i < splits; i += 64) l = fmaf(frame_weight(ml[2 * i], top), ml[2 * i + 1], l);
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off, 64);
   // D / 64 elements a lane where that is whole, the lanes past D idle otherwise
@@ -1075,12 +1101,13 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, in
   float o[kPer];
 #pragma unroll
   for (int e = 0; e < kPer; ++e) o[e] = 0.0f;
+  const float* part = a.part + id * a.splits * D;
 #pragma unroll 4
-  for (int i = 0; i < parts; ++i) {
-    const float w = frame_weight(a.part_ml[2 * part_at(i)], top);
+  for (int i = 0; i < splits; ++i) {
+    const float w = frame_weight(ml[2 * i], top);
 #pragma unroll
     for (int e = 0; e < kPer; ++e)
-      if (kPer * lane + e < D) o[e] = fmaf(w, a.part[part_at(i) * D + kPer * lane + e], o[e]);
+      if (kPer * lane + e < D) o[e] = fmaf(w, part[(int64_t)i * D + kPer * lane + e], o[e]);
   }
 #pragma unroll
   for (int e = 0; e < kPer; ++e)

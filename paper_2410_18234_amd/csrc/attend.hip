@@ -89,7 +89,7 @@ hipError_t attend_launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t total = a.T * a.heads * a.group;  // (at most 2^16: calls of more rows are not split)
-  attend_join_kernel<D, BF><<<(unsigned)((total + 3) / 4), 256, 0, st>>>(a, 16 * p.mt, total, 0);
+  attend_join_kernel<D, BF><<<(unsigned)((total + 3) / 4), 256, 0, st>>>(a, 16 * p.mt, total);
   return hipGetLastError();
 }
 

@@ -4,6 +4,7 @@
 // sequences; each sequence's own tokens follow, with the kernels of attend.h for both.  Each part of a row is its
 // maximum, sum and weighted values in the same frame, which the last launch joins.
 #include "attend.h"
+#include <stdlib.h>
 
 namespace mdss {
 
@@ -109,13 +110,328 @@ __global__ __launch_bounds__(NT) void shared_kernel(const SharedArgs a) {
 }
 
 // ---------------------------------------------------------------- attention
+// Few rows: four waves that take the same rows against tiles in turn (a prefix; own tokens of few sequences), or a wave for each
+// (sequence, head), which has no partners to wait for and to join: 2048 sequences of one token of their own past the prefix.
+template <int D, bool BF, int MT, int NW>
+__device__ __forceinline__ void shared_rows(const AttendArgs& a, const Place& p, float* joined, float* joined_ml,
+                                            typename Elem<BF>::vec* queries) {
+  if (MT > 1 && p.rows <= 16)
+    attend_rows<D, BF, 1, NW>(a, p, joined, joined_ml, queries);
+  else
+    attend_rows<D, BF, MT, NW>(a, p, joined, joined_ml, queries);
+}
+template <int D, bool BF, int MT>
+__global__ __launch_bounds__(256, D > 128 ? 1 : MT == 2 || D > 96 ? 2 : D == 96 ? 3 : 4) void attend_shared_kernel(const AttendArgs a) {
+  using vec = typename Elem<BF>::vec;
+  constexpr int kQueries = MT * D / 32 * 64, kJoined = 4 * joined_part(D) + 4 * 16 * 2;
+  constexpr int kTogether = kJoined * 4 + kQueries * 16, kApart = 4 * kQueries * 16;
+  __shared__ __align__(16) char lds[kTogether > kApart ? kTogether : kApart];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t block = a.block0 + blockIdx.x;
+  Place p;
+  if (block >= a.pre_blocks && a.own_waves == 1) {
+    if (attend_place<true>(a, 16 * MT, lane, p, a.pre_blocks + (block - a.pre_blocks) * 4 + wave))
+      shared_rows<D, BF, MT, 1>(a, p, nullptr, nullptr, reinterpret_cast<vec*>(lds) + wave * kQueries);
+  } else if (attend_place<true>(a, 16 * MT, lane, p, block)) {
+    float* joined = reinterpret_cast<float*>(lds);
+    shared_rows<D, BF, MT, 4>(a, p, joined, joined + 4 * joined_part(D), reinterpret_cast<vec*>(lds + kJoined * 4));
+  }
+}
+
+// A prefix under many rows: four waves take different rows (MT tiles of 16 each) against the same tiles of 64 tokens, widened into LDS once for
+// all of them.  The rows see all of the prefix, in whole tiles: nothing is masked but missing pages.  A tile is two steps: softmax and
+// staging, then the products of its values and of the next one's keys, with their operands read ahead; the two waves of a SIMD,
+// of two workgroups, fill each other's steps.
+template <int D, bool BF, int MT>
+__global__ __launch_bounds__(256, 2) void attend_prefix_kernel(const AttendArgs a) {
+  using E = Elem<BF>;
+  using vec = typename E::vec;
+  constexpr int kSteps = D / 32, kWhole = D / 64, kTiles = D / 16;
+  constexpr bool kHalf = D % 64 != 0;
+  constexpr int kValue = (kTiles + 3) / 4;  // a wave's 16-byte loads: keys of its quarter tt = wave, and these of the values
+  constexpr int kTile = 4 * kSteps * 64;  // keys (tt, step); values (dt, half)
+  __shared__ __align__(16) vec key_tile[kTile];
+  __shared__ __align__(16) f16x8 value_tile[kTile];  // (2 kTiles = 4 kSteps)
+  __shared__ int again_any[4];
+
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Place p;
+  if (!attend_place<true>(a, 64 * MT, lane, p, a.block0 + blockIdx.x)) return;
+  const int row0 = p.tile * 64 * MT + wave * 16 * MT, h = p.h;
+  const int t_begin = p.begin(), tiles = p.end(p.len >> 6) - t_begin;
+  if (tiles <= 0) return;  // (another split than the first, which has them all)
+
+  vec qf[MT][kSteps];
+  int lim[MT];
+  load_queries<D, BF, MT>(a, p, row0, m, g, qf, lim);
+  const bool idle = row0 >= p.rows;
+  f32x4 acc[kTiles][MT];
+  float M[MT], l[MT];
+  u16x2 least = {0x3c00, 0x3c00};
+  float ve_least = INFINITY, ve_most = -INFINITY;
+
+  const PageWalk walk(a, p);
+  const int64_t lane_v = m * 16;
+  const auto key_page = [&](int t) { return walk.page(4 * (t_begin + t) + (m >> 2)); };
+  const auto value_page = [&](int t) { return walk.page(4 * (t_begin + t) + g); };
+  u32x4 key_stage[kWhole], value_stage[kValue];
+  u32x2 key_half;
+  // (tiles past the last one: the last page again)
+  const auto load_keys = [&](int page, int t) __attribute__((always_inline)) {
+    bool ok;
+    const uint8_t* at = walk.unit(a.k, walk.valid(page, ok), 4 * (t_begin + t) + (m >> 2), 16 * D) + (m & 3) * 16 + wave * 64;
+#pragma unroll
+    for (int i = 0; i < kWhole; ++i) key_stage[i] = *reinterpret_cast<const u32x4*>(at + i * 1024 + g * 256);
+    if (kHalf) key_half = *reinterpret_cast<const u32x2*>(at + (4 * kWhole + (g >> 1)) * 256 + (g & 1) * 8);
+  };
+  const auto load_values = [&](int page, int t) __attribute__((always_inline)) {
+    const uint8_t* at = walk.unit(a.v, page, 4 * (t_begin + t) + g, 16 * D) + lane_v;
+#pragma unroll
+    for (int j = 0; j < kValue; ++j)
+      if (kTiles % 4 == 0 || wave * kValue + j < kTiles) value_stage[j] = *reinterpret_cast<const u32x4*>(at + (wave * kValue + j) * 256);
+  };
+  const auto put_keys = [&]() __attribute__((always_inline)) {
+    vec* to = key_tile + wave * kSteps * 64 + lane;
+#pragma unroll
+    for (int i = 0; i < kWhole; ++i) {
+      to[2 * i * 64] = E::widen(key_stage[i][0], key_stage[i][1]);
+      to[(2 * i + 1) * 64] = E::widen(key_stage[i][2], key_stage[i][3]);
+    }
+    if (kHalf) to[(kSteps - 1) * 64] = E::widen(key_half[0], key_half[1]);
+  };
+  const auto put_values = [&](bool ok) __attribute__((always_inline)) {
+    if (__ballot(ok) != ~0ull) {  // (any bytes in place of a page that is not there)
+#pragma unroll
+      for (int j = 0; j < kValue; ++j) value_stage[j] = low_bytes(value_stage[j], ok ? 16 : 0);
+    }
+    f16x8* to = value_tile + wave * kValue * 128 + lane;
+#pragma unroll
+    for (int j = 0; j < kValue; ++j)
+      if (kTiles % 4 == 0 || wave * kValue + j < kTiles) {
+        to[2 * j * 64] = Elem<false>::widen(value_stage[j][0], value_stage[j][1]);
+        to[(2 * j + 1) * 64] = Elem<false>::widen(value_stage[j][2], value_stage[j][3]);
+      }
+  };
+
+  const auto pass = [&](auto flag, bool mine) __attribute__((always_inline)) {
+    constexpr bool PRECISE = decltype(flag)::value;
+    if (mine) {
+#pragma unroll
+      for (int r = 0; r < MT; ++r) {
+        M[r] = -INFINITY;
+        l[r] = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      }
+    }
+    bool far = false;
+    f32x4 sc[4][MT];
+    f16x8 pf[MT][2];
+    f16x8 left[PRECISE ? MT : 1][2];
+    float back[PRECISE ? MT : 1];
+    int ke, ve, pv;
+    bool ok;
+    const auto load_exponents = [&](int page) __attribute__((always_inline)) {
+      pv = walk.valid(page, ok);
+      ke = a.k_exp[(int64_t)pv * a.heads + h];
+      ve = a.v_exp[(int64_t)pv * a.heads + h];
+    };
+    // Products by chunks of kSteps operands, the next chunk's on their way from LDS meanwhile (the compiler would wait for each pair).
+    // Four sums are taken in turn: chunks 0 .. 3 are the values' (two d tiles, both halves), 4 .. 7 the keys' (two token tiles, the steps).
+    u32x4 operand[2][kSteps];
+    const auto fetch = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        const int f = (c & 3) * kSteps + i;
+        const int at = c < 4 ? 2 * (f / 4 * 2 + (f & 1)) + f % 4 / 2 : (f / (2 * kSteps) * 2 + (f & 1)) * kSteps + f % (2 * kSteps) / 2;
+        operand[c & 1][i] = c < 4 ? __builtin_bit_cast(u32x4, value_tile[at * 64 + lane]) : __builtin_bit_cast(u32x4, key_tile[at * 64 + lane]);
+      }
+    };
+    const auto multiply = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        const int f = (c & 3) * kSteps + i;
+#pragma unroll
+        for (int r = 0; r < MT; ++r) {
+          if (c < 4) {
+            f32x4& sum = acc[f / 4 * 2 + (f & 1)][r];
+            sum = Elem<false>::mfma(__builtin_bit_cast(f16x8, operand[c & 1][i]), pf[r][f % 4 / 2], sum);
+          } else {
+            f32x4& sum = sc[f / (2 * kSteps) * 2 + (f & 1)][r];
+            const int st = f % (2 * kSteps) / 2;
+            sum = E::mfma(__builtin_bit_cast(vec, operand[c & 1][i]), qf[r][st], st == 0 ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : sum);
+          }
+        }
+      }
+    };
+    const auto multiply_chunks = [&](int from, int to) __attribute__((always_inline)) {
+      fetch(from);
+#pragma unroll
+      for (int c = from; c < to; ++c) {
+        if (c + 1 < to) fetch(c + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(c);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    load_keys(key_page(0), 0);
+    put_keys();
+    load_exponents(value_page(0));
+    load_keys(key_page(1), 1);
+    load_values(pv, 0);
+    int next_key = key_page(2), next_value = value_page(1);
+    __syncthreads();
+    if (mine) multiply_chunks(4, 8);
+    __syncthreads();
+    for (int t = 0; t < tiles; ++t) {
+      const bool ok_now = ok;
+      float c_g = a.scale_log2 * pow2i(ok_now ? ke : 0), ve_g = ok_now ? (float)ve : 0.0f, inv_v = pow2i(ok_now ? -ve : 0);
+      asm volatile("" : "+v"(c_g), "+v"(ve_g), "+v"(inv_v));  // (before the next tile's exponents are loaded, into the same registers)
+      if (mine) {
+        const bool masked = __ballot(ok_now) != ~0ull;
+        int upto[MT];
+#pragma unroll
+        for (int r = 0; r < MT; ++r) upto[r] = ok_now ? 16 : 0;
+        float alpha[MT];
+        bool grown;
+        if constexpr (PRECISE) {
+          grown = raise_frame<MT, true, true>(sc, c_g, ve_g, upto, M, l, alpha, far);
+          if (far)
+            weigh_far<MT>(sc, c_g, ve_g, inv_v, upto, M, l, pf);
+          else
+            weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf, least);
+        } else {
+          ve_least = fminf(ve_least, ve_g);
+          ve_most = fmaxf(ve_most, ve_g);
+          grown = masked ? raise_frame<MT, true, false>(sc, c_g, ve_g, upto, M, l, alpha, far)
+                         : raise_frame<MT, false, false>(sc, c_g, ve_g, upto, M, l, alpha, far);
+          if (masked)
+            weigh<MT, true>(sc, c_g, ve_g, inv_v, upto, M, l, pf, least);
+          else
+            weigh<MT, false>(sc, c_g, ve_g, inv_v, upto, M, l, pf, least);
+        }
+        if (grown) {
+#pragma unroll
+          for (int r = 0; r < MT; ++r)
+#pragma unroll
+            for (int dt = 0; dt < kTiles; ++dt) acc[dt][r] *= alpha[r];
+        }
+        if constexpr (PRECISE) {
+#pragma unroll
+          for (int r = 0; r < MT; ++r) left_of_low<MT>(sc, r, c_g, ve_g, upto[r], M[r], far, left[r], back[r]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      put_keys();
+      put_values(ok_now);
+      load_exponents(next_value);
+      load_keys(next_key, t + 2);
+      load_values(pv, t + 1);
+      next_key = key_page(t + 3);
+      next_value = value_page(t + 2);
+      __syncthreads();
+      if (mine) {
+        __builtin_amdgcn_s_setprio(1);
+if constexpr (PRECISE) {
+          multiply_chunks(0, 4);
+#pragma unroll
+          for (int r = 0; r < MT; ++r)
+            add_left<MT, kTiles>(left[r], back[r], r, acc, [&](int dt, int hs) {
+              f16x8 v = value_tile[(2 * dt + hs) * 64 + lane];
+              asm volatile("" : "+v"(v));  // (read again, not held from above)
+              return v;
+            });
+          multiply_chunks(4, 8);
+        } else {
+          multiply_chunks(0, 8);
+        }
+        __builtin_amdgcn_s_setprio(0);
+      }
+      __syncthreads();
+    }
+  };
+  pass(Flag<false>{}, !idle);
+  const bool again = !idle && lacks<MT, kTiles>(acc, M, lim, least, ve_least, ve_most, 64.0f * tiles);
+  if (lane == 0) again_any[wave] = again;
+  __syncthreads();
+  if (again_any[0] | again_any[1] | again_any[2] | again_any[3]) pass(Flag<true>{}, again);
+  if (idle) return;
+#pragma unroll
+  for (int r = 0; r < MT; ++r) l[r] = row_sum4(l[r]);
+  write_rows<D, BF, MT>(a, p, row0, m, g, acc, M, l);
+}
+
+// Joins a row's parts: those of the tokens it shares, then those of its sequence's own.  A wave has one token and as many of its heads as
+// fit, eight elements a lane, so what the rows of a token have in common is found once.
+template <int D, bool BF>
+__global__ __launch_bounds__(256) void shared_join_kernel(const AttendArgs a, int rows_tile, int chunks, int64_t first_token) {
+  using vec = typename Elem<BF>::vec;
+  using one = typename Elem<BF>::one;
+  constexpr int kLanes = D <= 64 ? 8 : D <= 128 ? 16 : 32;  // of a row (96: the last four idle)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t item = blockIdx.x * 4 + wave, token = item / (uint32_t)chunks;
+  const int64_t t = first_token + token;
+  if (t >= a.T) return;
+  const int heads_q = a.heads * a.group;
+  const int hq = (int)(item - token * chunks) * (64 / kLanes) + lane / kLanes, at = lane % kLanes * 8;
+  int s, n;
+  int64_t start;
+  if (a.starts) {
+    s = slot_sequence(a.starts, a.S, t, 1, 1, 0, lane);
+    start = a.starts[s];
+    n = (int)(a.starts[s + 1] - start);
+  } else {
+    n = (int)(a.T / a.S);
+    s = (int)((uint32_t)t / (uint32_t)n);
+    start = (int64_t)s * n;
+  }
+  if (start < 0 || t < start || t >= start + n || start + n > a.T) return;  // a token of no sequence
+  if (hq >= heads_q || at >= D) return;
+  const int length = a.lengths[s], before = length - n;
+  const int first = shared_tokens(a, s, before) >> 6;
+  const int prefix = min(a.pre_splits, (first + a.pre_split_tiles - 1) / a.pre_split_tiles);
+  int parts = prefix + 1;
+  if (a.splits > 1) {  // the splits that had tokens for the row's tile
+    const int rows = n * a.group, row = (int)(t - start) * a.group + hq % a.group, row0 = row / rows_tile * rows_tile;
+    const int len = max(0, min(length, (int)min(a.width << a.page_shift, (int64_t)INT32_MAX)));
+    const int lim_hi = min(len, before + min(rows - 1, row0 + rows_tile - 1) / a.group + 1);
+    const int tiles = (lim_hi > 0 ? (lim_hi + 63) >> 6 : 0) - first;
+    parts = prefix + max(1, min(a.splits, (tiles + a.split_tiles - 1) / a.split_tiles));
+  }
+  const int64_t id = t * heads_q + hq, base = id * (a.pre_splits + a.splits);
+  const auto part_at = [&](int i) { return base + (i < prefix ? i : i - prefix + a.pre_splits); };
+  float top = -INFINITY, l = 0.0f;
+#pragma unroll 4
+  for (int i = 0; i < parts; ++i) top = fmaxf(top, a.part_ml[2 * part_at(i)]);
+  f32x4 lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
+#pragma unroll 4
+  for (int i = 0; i < parts; ++i) {
+    const int64_t k = part_at(i);
+    const float w = frame_weight(a.part_ml[2 * k], top);
+    l = fmaf(w, a.part_ml[2 * k + 1], l);
+    const f32x4* x = reinterpret_cast<const f32x4*>(a.part + k * D + at);
+    lo = __builtin_elementwise_fma(f32x4{w, w, w, w}, x[0], lo);
+    hi = __builtin_elementwise_fma(f32x4{w, w, w, w}, x[1], hi);
+  }
+  vec o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    o[e] = (one)(l == 0.0f ? 0.0f : lo[e] / l);
+    o[4 + e] = (one)(l == 0.0f ? 0.0f : hi[e] / l);
+  }
+  *reinterpret_cast<vec*>(static_cast<one*>(a.out) + id * D + at) = o;
+  if (a.lse && at == 0) a.lse[id] = log_sum(top, l);
+}
+
 struct SharedPlan {
   int mt, pre_mt;          // row tiles of a wave, for the sequences' own tokens and for the prefixes
   bool wide, pre_wide;     // whether the waves take different rows
   int per_seq;
   int64_t slots, pre_slots;
   int splits, split_tiles, pre_splits, pre_split_tiles;
-  bool one_launch() const { return wide == pre_wide && mt == pre_mt; }
+  int own_waves;  // waves that share a sequence's rows (few rows)
+  bool one_launch() const { return !wide && !pre_wide; }
 };
 
 int64_t at_most(int64_t hint, int64_t most) { return hint > 0 && hint < most ? hint : most; }
@@ -134,15 +450,12 @@ void cut(int64_t tiles, int64_t splits, int* out_splits, int* out_tiles) {
 SharedPlan shared_plan(const CacheView& c, int64_t T, int64_t S, int64_t G, int64_t width, int group, bool uniform, int64_t max_new,
                        int64_t max_group, int64_t max_shared, int64_t max_own) {
   SharedPlan p;
-  const int most = c.d > 128 ? 2 : 4;
   const int64_t n = uniform ? T / S : at_most(max_new, T), all = at_most(max_group, T);
-  const auto kind = [&](int64_t rows, int& mt, bool& wide) {
-    wide = rows > 16 * most;
-    mt = wide ? (c.d > 128 ? 1 : 2) : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  };
-  kind(n * group, p.mt, p.wide);
-  kind(all * group, p.pre_mt, p.pre_wide);
-  if (p.wide == p.pre_wide) p.mt = p.pre_mt = p.mt > p.pre_mt ? p.mt : p.pre_mt;
+  p.wide = n * group > 64;
+  p.mt = p.wide ? (c.d > 128 ? 1 : 2) : n * group <= 16 ? 1 : 2;
+  p.pre_wide = all * group > 32;
+  p.pre_mt = p.pre_wide ? (c.d > 128 || all * group <= 64 ? 1 : 2) : all * group <= 16 ? 1 : 2;
+  if (p.one_launch()) p.mt = p.pre_mt = p.mt > p.pre_mt ? p.mt : p.pre_mt;
   const int tile = (p.wide ? 64 : 16) * p.mt, pre_tile = (p.pre_wide ? 64 : 16) * p.pre_mt;
   p.per_seq = uniform ? (int)((n * group + tile - 1) / tile) : 0;
   p.slots = uniform ? S * p.per_seq : T * group / tile + S;
@@ -152,50 +465,65 @@ SharedPlan shared_plan(const CacheView& c, int64_t T, int64_t S, int64_t G, int6
   const auto full = [&](int64_t sets, int64_t rows) { return (sets > (T * group + rows - 1) / rows ? sets : (T * group + rows - 1) / rows) * c.heads; };
   const int64_t own = full(S, tile), pre = full(G > 0 ? G : 1, pre_tile);
   // A prefix: as many workgroups as the CUs hold, of at least four tiles (one a wave) or, where the waves take different rows, eight.
-  int64_t pre_splits = 512 / pre;
-  const int64_t least = p.pre_wide ? 8 : 4;
+  const auto knob = [](const char* n, int64_t d) { const char* e = getenv(n); return e ? (int64_t)atoll(e) : d; };
+  int64_t pre_splits = knob("PRE", 512) / pre;
+  const int64_t least = knob("LEAST", p.pre_wide ? 8 : 4);
   if (pre_splits > pre_tiles / least) pre_splits = pre_tiles / least;
   cut(pre_tiles, pre_splits, &p.pre_splits, &p.pre_split_tiles);
-  int64_t splits = 512 / own;
+  int64_t splits = knob("OWN", 512) / own;
   if (splits > tiles / 8) splits = tiles / 8;
+  p.own_waves = 4;
+  if (!p.wide && own >= knob("OWN1", 1024)) {
+    p.own_waves = 1;
+    splits = 1;
+  }
   cut(tiles, splits, &p.splits, &p.split_tiles);
   return p;
 }
 
 template <typename Kernel>
-hipError_t shared_blocks(Kernel kernel, AttendArgs a, int64_t from, int64_t to, hipStream_t st) {
-  constexpr int64_t most = (1 << 24) - 1;  // (a dimension of a launch holds less than 2^32 threads)
+hipError_t shared_blocks(Kernel kernel, int threads, AttendArgs a, int64_t from, int64_t to, hipStream_t st) {
+  const int64_t most = (1LL << 32) / threads - 1;  // (a dimension of a launch holds less than 2^32 threads)
   for (; from < to; from += most) {
     a.block0 = from;
-    kernel<<<(unsigned)(to - from < most ? to - from : most), 256, 0, st>>>(a);
+    kernel<<<(unsigned)(to - from < most ? to - from : most), threads, 0, st>>>(a);
   }
   return hipGetLastError();
 }
 
+// Few rows: prefixes and own tokens in one launch, or one of them alone.
 template <int D, bool BF>
-hipError_t shared_part(const AttendArgs& a, bool wide, int mt, int64_t from, int64_t to, hipStream_t st) {
-  if (wide) return shared_blocks(attend_wide_kernel<D, BF, D == 256 ? 1 : 2, true>, a, from, to, st);
-  if (mt == 1) return shared_blocks(attend_kernel<D, BF, 1, true>, a, from, to, st);
+hipError_t shared_few(const AttendArgs& a, int mt, int64_t from, int64_t to, hipStream_t st) {
+  return mt == 1 ? shared_blocks(attend_shared_kernel<D, BF, 1>, 256, a, from, to, st)
+                 : shared_blocks(attend_shared_kernel<D, BF, 2>, 256, a, from, to, st);
+}
+template <int D, bool BF>
+hipError_t shared_prefix(const AttendArgs& a, int mt, hipStream_t st) {
   if constexpr (D <= 128) {
-    if (mt == 4) return shared_blocks(attend_kernel<D, BF, 4, true>, a, from, to, st);
+    if (mt == 2) return shared_blocks(attend_prefix_kernel<D, BF, 2>, 256, a, 0, a.pre_blocks, st);
   }
-  return shared_blocks(attend_kernel<D, BF, 2, true>, a, from, to, st);
+  return shared_blocks(attend_prefix_kernel<D, BF, 1>, 256, a, 0, a.pre_blocks, st);
 }
 
 template <int D, bool BF>
 hipError_t shared_launch(const AttendArgs& a, const SharedPlan& p, hipStream_t st) {
-  const int64_t blocks = a.pre_blocks + p.slots * a.heads * p.splits;
-  hipError_t e;
+  const int64_t own = p.slots * a.heads * p.splits, blocks = a.pre_blocks + (p.own_waves == 1 ? (own + 3) / 4 : own);
+  constexpr int MT = D == 256 ? 1 : 2;
+  hipError_t e = hipSuccess;
   if (p.one_launch()) {
-    e = shared_part<D, BF>(a, p.wide, p.mt, 0, blocks, st);
+    e = shared_few<D, BF>(a, p.mt, 0, blocks, st);
   } else {
-    e = shared_part<D, BF>(a, p.pre_wide, p.pre_mt, 0, a.pre_blocks, st);
-    if (e == hipSuccess) e = shared_part<D, BF>(a, p.wide, p.mt, a.pre_blocks, blocks, st);
+    e = p.pre_wide ? shared_prefix<D, BF>(a, p.pre_mt, st) : shared_few<D, BF>(a, p.pre_mt, 0, a.pre_blocks, st);
+    if (e == hipSuccess)
+      e = p.wide ? shared_blocks(attend_wide_kernel<D, BF, MT, true>, 256, a, a.pre_blocks, blocks, st)
+                 : shared_few<D, BF>(a, p.mt, a.pre_blocks, blocks, st);
   }
-  const int64_t total = a.T * a.heads * a.group, most = 1LL << 25;
-  for (int64_t row = 0; e == hipSuccess && row < total; row += most) {
-    const int64_t rows = total - row < most ? total - row : most;
-    attend_join_kernel<D, BF, true><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a, (p.wide ? 64 : 16) * p.mt, row + rows, row);
+  constexpr int kRows = D <= 64 ? 8 : D <= 128 ? 4 : 2;  // of a wave
+  const int chunks = (a.heads * a.group + kRows - 1) / kRows;
+  const int64_t most = ((1LL << 24) - 1) * 4 / chunks;  // tokens of a launch
+  for (int64_t t = 0; e == hipSuccess && t < a.T; t += most) {
+    const int64_t n = a.T - t < most ? a.T - t : most;
+    shared_join_kernel<D, BF><<<(unsigned)((n * chunks + 3) / 4), 256, 0, st>>>(a, (p.wide ? 64 : 16) * p.mt, chunks, t);
     e = hipGetLastError();
   }
   return e;
@@ -238,6 +566,7 @@ hipError_t launch_cache_attention_shared(const CacheView& c, int layer, const vo
   a.pre_slots = (int)p.pre_slots;
   a.pre_splits = p.pre_splits;
   a.pre_split_tiles = p.pre_split_tiles;
+  a.own_waves = p.own_waves;
   a.pre_blocks = p.pre_slots * c.heads * p.pre_splits;
   const bool bf = dtype == MDSS_BF16;
   switch (c.d) {
