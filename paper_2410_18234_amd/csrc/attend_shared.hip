@@ -4,7 +4,6 @@
 // sequences; each sequence's own tokens follow, with the kernels of attend.h for both.  Each part of a row is its
 // maximum, sum and weighted values in the same frame, which the last launch joins.
 #include "attend.h"
-#include <stdlib.h>
 
 namespace mdss {
 
@@ -451,42 +450,47 @@ SharedPlan shared_plan(const CacheView& c, int64_t T, int64_t S, int64_t G, int6
                        int64_t max_group, int64_t max_shared, int64_t max_own) {
   SharedPlan p;
   const int64_t n = uniform ? T / S : at_most(max_new, T), all = at_most(max_group, T);
+  const int64_t tokens = width << c.page_shift;
+  const int64_t tiles = (at_most(max_own, tokens) + 63) >> 6, pre_tiles = (at_most(max_shared, tokens) + 63) >> 6;
   p.wide = n * group > 64;
   p.mt = p.wide ? (c.d > 128 ? 1 : 2) : n * group <= 16 ? 1 : 2;
-  p.pre_wide = all * group > 32;
-  p.pre_mt = p.pre_wide ? (c.d > 128 || all * group <= 64 ? 1 : 2) : all * group <= 16 ? 1 : 2;
+  // Which kernel a prefix takes.  Up to 32 rows: the one bound by memory.  More than 64: the many-row one.  Between them the many-row kernel
+  // is the faster one by itself, but a launch of its own, behind which the sequences' own tokens wait: it is taken for long or many prefixes
+  // (64 rows of 128, 8 cache heads; few and many rows' kernel: 64 groups of 6016 tokens 387 and 226 us; 32 of up to 4000, 20 rows of
+  // each sequence's own: 64 and 71; 8 of 4000: 32 and 36; 64 of up to 1000: 52 and 53).
+  const int64_t rows = all * group;
+  p.pre_wide = rows > 64 || (rows > 32 && G * c.heads * pre_tiles >= 24576);
+  p.pre_mt = p.pre_wide ? (c.d > 128 || rows <= 64 ? 1 : 2) : rows <= 16 ? 1 : 2;
   if (p.one_launch()) p.mt = p.pre_mt = p.mt > p.pre_mt ? p.mt : p.pre_mt;
   const int tile = (p.wide ? 64 : 16) * p.mt, pre_tile = (p.pre_wide ? 64 : 16) * p.pre_mt;
   p.per_seq = uniform ? (int)((n * group + tile - 1) / tile) : 0;
   p.slots = uniform ? S * p.per_seq : T * group / tile + S;
   p.pre_slots = G > 0 ? T * group / pre_tile + G : 0;
-  const int64_t tokens = width << c.page_shift;
-  const int64_t tiles = (at_most(max_own, tokens) + 63) >> 6, pre_tiles = (at_most(max_shared, tokens) + 63) >> 6;
   const auto full = [&](int64_t sets, int64_t rows) { return (sets > (T * group + rows - 1) / rows ? sets : (T * group + rows - 1) / rows) * c.heads; };
   const int64_t own = full(S, tile), pre = full(G > 0 ? G : 1, pre_tile);
-  // A prefix: as many workgroups as the CUs hold, of at least four tiles (one a wave) or, where the waves take different rows, eight.
-  const auto knob = [](const char* n, int64_t d) { const char* e = getenv(n); return e ? (int64_t)atoll(e) : d; };
-  int64_t pre_splits = knob("PRE", 512) / pre;
-  const int64_t least = knob("LEAST", p.pre_wide ? 8 : 4);
+  // A prefix: as many workgroups as the CUs hold (the many-row kernel's with 16 rows a wave: half again, twice evens out unlike lengths: 64
+  // groups of 12 rows of 4 heads, up to 6016 tokens: 162 us, 173 with 512), of at least four tiles (one a wave) or, where the waves take
+  // different rows, eight.  (16 groups of 32 rows, up to 6000 tokens: 512 workgroups 52 us, 1024 60, 256 69; 2048 rows over 8192 tokens: 512
+  // 167 us, 1024 181.)
+  int64_t pre_splits = (p.pre_wide && p.pre_mt == 1 && c.d <= 128 ? 1024 : 512) / pre;
+  const int64_t least = p.pre_wide ? 8 : 4;
   if (pre_splits > pre_tiles / least) pre_splits = pre_tiles / least;
   cut(pre_tiles, pre_splits, &p.pre_splits, &p.pre_split_tiles);
-  int64_t splits = knob("OWN", 512) / own;
+  // Own tokens: a wave for each (sequence, head) where there are enough of them (128 sequences of up to 150 tokens, 8 heads: 21.7 us, 24.1 with
+  // four waves each; of 600: 44 and 47.5; 32 sequences of 600: 22.5 and 20.4), else four waves, split as long as CUs are left.
+  p.own_waves = !p.wide && own >= 1024 ? 1 : 4;
+  int64_t splits = p.own_waves == 1 ? 1 : 512 / own;
   if (splits > tiles / 8) splits = tiles / 8;
-  p.own_waves = 4;
-  if (!p.wide && own >= knob("OWN1", 1024)) {
-    p.own_waves = 1;
-    splits = 1;
-  }
   cut(tiles, splits, &p.splits, &p.split_tiles);
   return p;
 }
 
 template <typename Kernel>
-hipError_t shared_blocks(Kernel kernel, int threads, AttendArgs a, int64_t from, int64_t to, hipStream_t st) {
-  const int64_t most = (1LL << 32) / threads - 1;  // (a dimension of a launch holds less than 2^32 threads)
+hipError_t shared_blocks(Kernel kernel, AttendArgs a, int64_t from, int64_t to, hipStream_t st) {
+  constexpr int64_t most = (1 << 24) - 1;  // (a dimension of a launch holds less than 2^32 threads)
   for (; from < to; from += most) {
     a.block0 = from;
-    kernel<<<(unsigned)(to - from < most ? to - from : most), threads, 0, st>>>(a);
+    kernel<<<(unsigned)(to - from < most ? to - from : most), 256, 0, st>>>(a);
   }
   return hipGetLastError();
 }
@@ -494,28 +498,27 @@ hipError_t shared_blocks(Kernel kernel, int threads, AttendArgs a, int64_t from,
 // Few rows: prefixes and own tokens in one launch, or one of them alone.
 template <int D, bool BF>
 hipError_t shared_few(const AttendArgs& a, int mt, int64_t from, int64_t to, hipStream_t st) {
-  return mt == 1 ? shared_blocks(attend_shared_kernel<D, BF, 1>, 256, a, from, to, st)
-                 : shared_blocks(attend_shared_kernel<D, BF, 2>, 256, a, from, to, st);
+  return mt == 1 ? shared_blocks(attend_shared_kernel<D, BF, 1>, a, from, to, st)
+                 : shared_blocks(attend_shared_kernel<D, BF, 2>, a, from, to, st);
 }
 template <int D, bool BF>
 hipError_t shared_prefix(const AttendArgs& a, int mt, hipStream_t st) {
   if constexpr (D <= 128) {
-    if (mt == 2) return shared_blocks(attend_prefix_kernel<D, BF, 2>, 256, a, 0, a.pre_blocks, st);
+    if (mt == 2) return shared_blocks(attend_prefix_kernel<D, BF, 2>, a, 0, a.pre_blocks, st);
   }
-  return shared_blocks(attend_prefix_kernel<D, BF, 1>, 256, a, 0, a.pre_blocks, st);
+  return shared_blocks(attend_prefix_kernel<D, BF, 1>, a, 0, a.pre_blocks, st);
 }
 
 template <int D, bool BF>
 hipError_t shared_launch(const AttendArgs& a, const SharedPlan& p, hipStream_t st) {
-  const int64_t own = p.slots * a.heads * p.splits, blocks = a.pre_blocks + (p.own_waves == 1 ? (own + 3) / 4 : own);
-  constexpr int MT = D == 256 ? 1 : 2;
-  hipError_t e = hipSuccess;
+  const int64_t tasks = p.slots * a.heads * p.splits, blocks = a.pre_blocks + (p.own_waves == 1 ? (tasks + 3) / 4 : tasks);
+  hipError_t e;
   if (p.one_launch()) {
     e = shared_few<D, BF>(a, p.mt, 0, blocks, st);
   } else {
     e = p.pre_wide ? shared_prefix<D, BF>(a, p.pre_mt, st) : shared_few<D, BF>(a, p.pre_mt, 0, a.pre_blocks, st);
     if (e == hipSuccess)
-      e = p.wide ? shared_blocks(attend_wide_kernel<D, BF, MT, true>, 256, a, a.pre_blocks, blocks, st)
+      e = p.wide ? shared_blocks(attend_wide_kernel<D, BF, D == 256 ? 1 : 2, true>, a, a.pre_blocks, blocks, st)
                  : shared_few<D, BF>(a, p.mt, a.pre_blocks, blocks, st);
   }
   constexpr int kRows = D <= 64 ? 8 : D <= 128 ? 4 : 2;  // of a wave
