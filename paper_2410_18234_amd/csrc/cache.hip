@@ -72,101 +72,137 @@ struct AppendArgs {
   const uint16_t* q;
   uint16_t* q_out;
   int64_t q_st, q_sh, qo_st, qo_sh;
-  int group;  // query heads of a cache head (0: no queries)
+  int q_heads;  // query heads of a workgroup (0: no queries)
   bool q_al;
   bool halves;  // pairs lie half of the turned part apart, in whole pieces of 8
 };
 
-// Two pieces of 8 elements of a token, which a thread turns together: those at the same place of both halves of the turned part, or
-// neighbours (pairs side by side, halves that are not whole pieces, and what is not turned).
+// Two pieces of 8 elements of a token, which a thread turns together: those at the same place of both halves of the turned part, or (pairs
+// side by side, halves that are not whole pieces, and what is not turned) two that lie half of the rest apart, so that the
+// lanes of a load are next to each other.
 struct Bundle {
   int first, second;  // pieces of the token
   bool pairs;         // they are each other's pairs
 };
+template <int D>
 __device__ __forceinline__ Bundle bundle_of(const AppendArgs& a, int b) {
   const int half = a.halves ? a.rope.pairs >> 3 : 0;
   if (b < half) return {b, b + half, true};
-  return {2 * b, 2 * b + 1, false};  // (2 half + 2 (b - half))
+  return {b + half, b + D / 16, false};
 }
 
-// The bundle's elements times `scale` (a power of two, before anything that could pass fp32's range) at `position`, turned, in fp32.
-// at: the token's elements.
-template <bool BF>
-__device__ __forceinline__ void turn_bundle(const AppendArgs& a, const Bundle& b, double position, float scale, const uint16_t* at,
-                                            const u32x4& first, const u32x4& second, float (&x)[8], float (&y)[8]) {
-  using P = Pack<BF ? 1 : 2>;
-  P::open(first, x);
-  P::open(second, y);
+// The angles of a bundle: of its pairs, or (side by side) of the first piece's four pairs and then the second's; turned: how many of
+// each four lie in the turned part.  Halves that are not whole pieces have their angles found element by element (turn_pieces).
+struct Angles {
+  float c[8], s[8];
+  int turned[2];
+};
+__device__ __forceinline__ void angles_of(const AppendArgs& a, const Bundle& b, double position, Angles& g) {
+  const int pairs = a.rope.pairs, first = b.pairs ? 8 * b.first : 4 * b.first, second = b.pairs ? first + 4 : 4 * b.second;
+  g.turned[0] = min(max(pairs - first, 0), 4);
+  g.turned[1] = min(max(pairs - second, 0), 4);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    x[i] *= scale;
-    y[i] *= scale;
+  for (int i = 0; i < 4; ++i) turn(a.rope, position, a.rope.freq[min(first + i, pairs - 1)], g.c[i], g.s[i]);
+  if (g.turned[1] > 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) turn(a.rope, position, a.rope.freq[min(second + i, pairs - 1)], g.c[4 + i], g.s[4 + i]);
+  } else {
+#pragma unroll
+    for (int i = 4; i < 8; ++i) g.c[i] = g.s[i] = 0.0f;
   }
-  const int pairs = a.rope.pairs;
+}
+__device__ __forceinline__ void apply(const Bundle& b, const Angles& g, float (&x)[8], float (&y)[8]) {
   if (b.pairs) {
-    const double* f = a.rope.freq + 8 * b.first;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      float c, s;
-      turn(a.rope, position, f[i], c, s);
       const float u = x[i], v = y[i];
-      x[i] = turned_first(u, v, c, s);
-      y[i] = turned_second(u, v, c, s);
+      x[i] = turned_first(u, v, g.c[i], g.s[i]);
+      y[i] = turned_second(u, v, g.c[i], g.s[i]);
     }
     return;
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float& u = i < 4 ? x[2 * i] : y[2 * i - 8];
+    float& v = i < 4 ? x[2 * i + 1] : y[2 * i - 7];
+    const bool in = (i & 3) < g.turned[i >> 2];  // (selected: what lies outside is left as it is, whatever its neighbour holds)
+    const float first = turned_first(u, v, g.c[i], g.s[i]), second = turned_second(u, v, g.c[i], g.s[i]);
+    u = in ? first : u;
+    v = in ? second : v;
+  }
+}
+// Halves that are not whole pieces of 8: each element's pair is read from `at` (the token's elements).
+template <bool BF>
+__device__ __forceinline__ void turn_pieces(const AppendArgs& a, const Bundle& b, double position, float scale, const uint16_t* at, float (&x)[8],
+                                            float (&y)[8]) {
+  using P = Pack<BF ? 1 : 2>;
+  const int pairs = a.rope.pairs;
   const auto piece = [&](float (&z)[8], int d0) __attribute__((always_inline)) {
-    if (d0 >= 2 * pairs) return;
-    if (a.rope.interleaved) {
-#pragma unroll
-      for (int i = 0; i < 8; i += 2)
-        if (d0 + i < 2 * pairs) {
-          float c, s;
-          turn(a.rope, position, a.rope.freq[(d0 + i) >> 1], c, s);
-          const float u = z[i], v = z[i + 1];
-          z[i] = turned_first(u, v, c, s);
-          z[i + 1] = turned_second(u, v, c, s);
-        }
-    } else {
 #pragma unroll 1
-      for (int i = 0; i < 8; ++i) {
-        const int d = d0 + i;
-        if (d >= 2 * pairs) break;
-        float c, s;
-        const bool up = d >= pairs;
-        turn(a.rope, position, a.rope.freq[up ? d - pairs : d], c, s);
-        const float mine = P::widen(__builtin_bit_cast(typename P::one, at[d])) * scale,
-                    other = P::widen(__builtin_bit_cast(typename P::one, at[up ? d - pairs : d + pairs])) * scale;
-        const float to = up ? turned_second(other, mine, c, s) : turned_first(mine, other, c, s);
+    for (int i = 0; i < 8; ++i) {
+      const int d = d0 + i;
+      if (d >= 2 * pairs) break;
+      float c, s;
+      const bool up = d >= pairs;
+      turn(a.rope, position, a.rope.freq[up ? d - pairs : d], c, s);
+      const float mine = P::widen(__builtin_bit_cast(typename P::one, at[d])) * scale,
+                  other = P::widen(__builtin_bit_cast(typename P::one, at[up ? d - pairs : d + pairs])) * scale;
+      const float to = up ? turned_second(other, mine, c, s) : turned_first(mine, other, c, s);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = j == i ? to : z[j];
-      }
+      for (int j = 0; j < 8; ++j) z[j] = j == i ? to : z[j];
     }
   };
   piece(x, 8 * b.first);
   piece(y, 8 * b.second);
 }
+// Whether a bundle's pairs lie within it
+__device__ __forceinline__ bool by_angles(const AppendArgs& a) { return a.halves || a.rope.interleaved; }
+// A bundle past the turned part
+__device__ __forceinline__ bool plain(const AppendArgs& a, const Bundle& b) { return !b.pairs && 8 * b.first >= 2 * a.rope.pairs; }
 
-// The queries of `cnt` tokens from `tok` on (in their sequence from `pos` on), of the query heads of cache head h.
+// The queries of `cnt` tokens from `tok` on (in their sequence from `pos` on), heads part * q_heads ..: a thread has a bundle of a
+// token and goes over the heads, or some of them, two in flight; the angles are formed once for them.
 template <int D, bool BF, int NT>
-__device__ __forceinline__ void turn_queries(const AppendArgs& a, int h, int64_t tok, int64_t pos, int cnt) {
-  constexpr int kBundles = D / 16;
+__device__ __forceinline__ void turn_queries(const AppendArgs& a, int part, int64_t tok, int64_t pos, int cnt) {
+  using P = Pack<BF ? 1 : 2>;
+  constexpr int kBundles = D / 16, kFlight = 2;
   const int total = cnt * kBundles;
-  // threads that a bundle's heads are divided between
-  const int slices = total >= NT ? 1 : min(a.group, NT / total);
+  const int slices = total >= NT ? 1 : min(a.q_heads, NT / total);  // threads that a bundle's heads are divided between
   for (int e = threadIdx.x; e < total * slices; e += NT) {
     const int slice = e / total, rest = e - slice * total, i = rest / kBundles;
-    const Bundle b = bundle_of(a, rest - i * kBundles);
+    const Bundle b = bundle_of<D>(a, rest - i * kBundles);
     const double position = a.positions ? (double)a.positions[tok + i] : (double)(pos + i);
-    for (int j = slice; j < a.group; j += slices) {
-      const int64_t head = (int64_t)h * a.group + j;
-      const uint16_t* at = a.q + (tok + i) * a.q_st + head * a.q_sh;
-      float x[8], y[8];
-      turn_bundle<BF>(a, b, position, 1.0f, at, load8(at + 8 * b.first, a.q_al), load8(at + 8 * b.second, a.q_al), x, y);
-      uint16_t* to = a.q_out + (tok + i) * a.qo_st + head * a.qo_sh;
-      const u32x4 first = Pack<BF ? 1 : 2>::close(x), second = Pack<BF ? 1 : 2>::close(y);
-      *reinterpret_cast<u32x4*>(to + 8 * b.first) = first;
-      *reinterpret_cast<u32x4*>(to + 8 * b.second) = second;
+    const uint16_t* at = a.q + (tok + i) * a.q_st + (int64_t)part * a.q_heads * a.q_sh;
+    uint16_t* to = a.q_out + (tok + i) * a.qo_st + (int64_t)part * a.q_heads * a.qo_sh;
+    const bool by = by_angles(a), none = plain(a, b);
+    Angles g;
+    if (by && !none) angles_of(a, b, position, g);
+    for (int j0 = slice; j0 < a.q_heads; j0 += kFlight * slices) {
+      u32x4 first[kFlight], second[kFlight];
+#pragma unroll
+      for (int f = 0; f < kFlight; ++f) {
+        const uint16_t* from = at + (int64_t)min(j0 + f * slices, a.q_heads - 1) * a.q_sh;
+        first[f] = load8(from + 8 * b.first, a.q_al);
+        second[f] = load8(from + 8 * b.second, a.q_al);
+      }
+#pragma unroll
+      for (int f = 0; f < kFlight; ++f) {
+        const int j = j0 + f * slices;
+        if (j >= a.q_heads) continue;
+        if (!none) {
+          float x[8], y[8];
+          P::open(first[f], x);
+          P::open(second[f], y);
+          if (by)
+            apply(b, g, x, y);
+          else
+            turn_pieces<BF>(a, b, position, 1.0f, at + (int64_t)j * a.q_sh, x, y);
+          first[f] = P::close(x);
+          second[f] = P::close(y);
+        }
+        *reinterpret_cast<u32x4*>(to + (int64_t)j * a.qo_sh + 8 * b.first) = first[f];
+        *reinterpret_cast<u32x4*>(to + (int64_t)j * a.qo_sh + 8 * b.second) = second[f];
+      }
     }
   }
 }
@@ -242,7 +278,7 @@ __global__ __launch_bounds__(NT, 4) void append_kernel(const AppendArgs a) {
   const auto key_piece = [&](int j, int e) {
     if (!TURN) return e;
     const int t = e / (kLine / 2);
-    const Bundle b = bundle_of(a, e - t * (kLine / 2));
+    const Bundle b = bundle_of<D>(a, e - t * (kLine / 2));
     return t * kLine + (j & 1 ? b.second : b.first);
   };
   const auto key_place = [&](int j) { return TURN ? tid + NT * (j >> 1) : tid + NT * j; };
@@ -358,10 +394,25 @@ __global__ __launch_bounds__(NT, 4) void append_kernel(const AppendArgs a) {
   if constexpr (TURN) {
     const auto put_bundle = [&](int e, const u32x4& first, const u32x4& second) __attribute__((always_inline)) {
       const int i = e / (kLine / 2);
-      const Bundle b = bundle_of(a, e - i * (kLine / 2));
+      const Bundle b = bundle_of<D>(a, e - i * (kLine / 2));
       const double position = a.positions ? (double)a.positions[tok + i] : (double)(base + o + i);
       float x[8], y[8];
-      turn_bundle<BF>(a, b, position, kf, kx + (int64_t)i * a.key_st, first, second, x, y);
+      Pack<BF ? 1 : 2>::open(first, x);
+      Pack<BF ? 1 : 2>::open(second, y);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {  // (at once, by a power of two: what is turned stays within fp32's range)
+        x[j] *= kf;
+        y[j] *= kf;
+      }
+      if (!plain(a, b)) {
+        if (by_angles(a)) {
+          Angles g;
+          angles_of(a, b, position, g);
+          apply(b, g, x, y);
+        } else {
+          turn_pieces<BF>(a, b, position, kf, kx + (int64_t)i * a.key_st, x, y);
+        }
+      }
       u32x2 cx, cy;
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
@@ -1059,10 +1110,15 @@ hipError_t launch_cache_append(const CacheView& c, int layer, const void* key, c
     a.q_sh = turn->q_sh;
     a.qo_st = turn->qo_st;
     a.qo_sh = turn->qo_sh;
-    a.group = turn->group;
+    a.q_heads = turn->group;
     a.q_al = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && a.q_st % 8 == 0 && a.q_sh % 8 == 0;
   }
-  const dim3 grid((unsigned)slots, (unsigned)(a.group > 0 ? 2 * c.heads : c.heads));
+  // queries: the more heads a workgroup has the better it hides the chain before its tokens, as long as there are enough of them (prompts
+  // of 16 x up to 2048 tokens, 32 heads: 176 us with 4 each)
+  int q_parts = 0;
+  if (a.q_heads > 0)
+    for (q_parts = c.heads; q_parts % 2 == 0 && slots * q_parts / 2 >= 1024; q_parts /= 2) a.q_heads *= 2;
+  const dim3 grid((unsigned)slots, (unsigned)(c.heads + q_parts));
   // few tokens a page: a wave is enough
   const bool small = rows.T <= 2 * (int64_t)rows.S, bf = dtype == MDSS_BF16;
   switch (c.d) {
