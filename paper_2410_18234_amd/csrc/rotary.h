@@ -1,7 +1,8 @@
 // Rotary positions: a pair (u, v) of a head's elements at position t becomes m (u cos a - v sin a, u sin a + v cos a), a = t f.
 //
 // The angle is formed in fp64 (fp32 loses 2^-24 of t f, whole turns at far positions): t f in quarter turns, whose whole part picks
-// the quadrant and whose rest, within half a quarter turn, goes to fp32 and two Taylor series (to r^9 and r^10: below 2^-25 there).
+// the quadrant and whose rest, within half a quarter turn, goes to two fp32 and two Taylor series (to r^9 and r^10: below 2^-25 there),
+// whose last step is one rounding: cosine and sine are off by little more than that.
 #pragma once
 
 #include <stdint.h>
@@ -25,10 +26,13 @@ struct Rope {
 __device__ __forceinline__ void turn(const Rope& r, double position, double freq, float& c, float& s) {
   const double t = position * (freq * 0.63661977236758134308);  // quarter turns
   const double n = t + 6755399441055744.0;                      // 1.5 2^52: the nearest whole number in the low bits
-  const float x = (float)(t - (n - 6755399441055744.0)), z = x * x;
+  const double rest = t - (n - 6755399441055744.0);
+  const float x = (float)rest, low = (float)(rest - (double)x), z = x * x;
   const uint32_t k = (uint32_t)__builtin_bit_cast(uint64_t, n);
-  const float sx = x * fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.6044118478735982e-4f, -4.681754135318687e-3f), 7.969262624616704e-2f),
-                                    -0.6459640975062463f), 1.5707963267948966f);
+  // pi / 2 = 1.57079637 (in fp32) - 4.37113883e-8
+  const float higher = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.6044118478735982e-4f, -4.681754135318687e-3f), 7.969262624616704e-2f), -0.6459640975062463f),
+                            -4.3711388e-8f);
+  const float sx = fmaf(x, 1.5707964f, fmaf(low, 1.5707964f, x * higher));
   const float cx = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -2.5202042373060605e-5f, 9.192602748394264e-4f), -2.0863480763352960e-2f),
                                         0.2536695079010480f), -1.2337005501361697f), 1.0f);
   const float co = k & 1 ? sx : cx, si = k & 1 ? cx : sx;
