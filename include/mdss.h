@@ -646,7 +646,8 @@ typedef struct mdss_rope {
 /* out[t][h] = x[t][h] at positions[t] ([T] int32), for x [T][heads][head_dim] of
  * any mdss_dtype; token and head strides in elements, the last dimension
  * contiguous.  out may be x (with its strides; only the turned part is written
- * then), else it must not overlap it, and its strides are at least head_dim.
+ * then), else it must not overlap it; its rows lie apart, [T][heads] or [heads][T] in
+ * memory, at least head_dim from each other (else MDSS_EINVAL).
  * T in [0, 2^24], head_dim up to 65536, heads * head_dim < 2^31.  T = 0: nothing to do. */
 mdss_status mdss_rotary(const void* x, int64_t x_token_stride, int64_t x_head_stride, mdss_dtype dtype, int64_t T, int64_t heads,
                         int64_t head_dim, const int32_t* positions, const mdss_rope* rope, int32_t inverse, void* out,
@@ -696,7 +697,8 @@ mdss_status mdss_cache_shared(const mdss_cache* cache, int64_t T, const int32_t*
  * max_new (of a sequence), max_group (new tokens of a group), max_shared and
  * max_own (a sequence's tokens past the shared ones) are host-side hints on the
  * most there are (0: none); they choose how the work is cut.
- * workspace: at least mdss_workspace_bytes_attention_shared(...) bytes, 256-byte aligned. */
+ * workspace: at least mdss_workspace_bytes_attention_shared(...) bytes, 256-byte aligned: head_dim + 2 floats for
+ * each part of a row of T * heads_q, which are two and more (a call for new tokens by the few, not for long prompts). */
 size_t mdss_workspace_bytes_attention_shared(const mdss_cache* cache, int64_t T, int64_t S, int64_t G, int64_t width, int64_t heads_q,
                                              int32_t uniform, int64_t max_new, int64_t max_group, int64_t max_shared, int64_t max_own);
 mdss_status mdss_cache_attention_shared(const mdss_cache* cache, int32_t layer, const void* q, int64_t q_token_stride,

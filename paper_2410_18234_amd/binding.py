@@ -165,6 +165,12 @@ def _stream(device: torch.device):
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
+def _here(device: torch.device):
+    """Kernels are launched on the current device: tensors of another one are refused."""
+    if torch._C._cuda_getDevice() != device.index:
+        raise ValueError(f"the tensors are on {device}, which is not the current device")
+
+
 def _need(t: torch.Tensor, name: str, dtype: torch.dtype, shape: tuple, device: torch.device):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")

@@ -24,7 +24,7 @@ from typing import Optional
 
 import torch
 
-from .binding import _check, _need, _ptr, _stream, _ws_arg, load_library
+from .binding import _check, _here, _need, _ptr, _stream, _ws_arg, load_library
 from .rotary import Rotary, _rope
 
 _DTYPES = {torch.bfloat16: 1, torch.float16: 2}
@@ -144,6 +144,7 @@ def cache_append_rotary(cache: PagedCache, layer: int, k: torch.Tensor, v: torch
     The queries ``q [T][heads_q][head_dim]``, if given, are turned in the same launch: returned in ``q_out`` (a new tensor if
     None; never q itself), where tokens of no sequence are not written."""
     lib = load_library()
+    _here(cache.device)
     S, width = _rows(cache, starts, table, lengths)
     dev = cache.device
     _tokens(k, "k", cache)
@@ -213,6 +214,7 @@ def cache_shared(cache: PagedCache, T: int, starts: Optional[torch.Tensor], tabl
     leading pages that are the same in all of them, in whole multiples of ``max(64, page_size)``, 0 where that is less than
     ``least``.  A group's row: its first new token, its new tokens, its first row that takes part (-1: none), its shared tokens."""
     lib = load_library()
+    _here(cache.device)
     S, width = _rows(cache, starts, table, lengths)
     dev = cache.device
     if groups.dim() != 1 or not groups.numel():
@@ -237,6 +239,7 @@ def cache_attention_shared(q: torch.Tensor, cache: PagedCache, layer: int, start
     ``max_new`` (of a sequence), ``max_group`` (new tokens of a group), ``max_shared`` and ``max_own`` (a sequence's tokens past the
     shared ones) say how many there are at most (0: unknown); they only choose how the work is cut."""
     lib = load_library()
+    _here(cache.device)
     S, width = _rows(cache, starts, table, lengths)
     _tokens(q, "q", cache)
     T, heads_q = q.shape[0], q.shape[1]

@@ -505,6 +505,10 @@ mdss_status mdss_rotary(const void* x, int64_t x_token_stride, int64_t x_head_st
   if (dtype != MDSS_F32 && dtype != MDSS_BF16 && dtype != MDSS_F16) return MDSS_EUNSUPPORTED;
   if (x_token_stride < 0 || x_head_stride < 0 || (T > 1 && out_token_stride < head_dim) || (heads > 1 && out_head_stride < head_dim))
     return MDSS_EINVAL;
+  // (no two rows of out in one place: tokens lie past each other's heads, or heads past each other's tokens)
+  if (T > 1 && heads > 1 && (out_token_stride - head_dim) / (heads - 1) < out_head_stride &&
+      (out_head_stride - head_dim) / (T - 1) < out_token_stride)
+    return MDSS_EINVAL;
   if (T == 0) return MDSS_OK;
   if (!x || !out || !positions || !rope->frequencies) return MDSS_EINVAL;
   if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(out)) & (dtype == MDSS_F32 ? 3 : 1)) return MDSS_EINVAL;

@@ -98,8 +98,8 @@ __global__ __launch_bounds__(NT) void shared_kernel(const SharedArgs a) {
     shared = (int)(min((int64_t)common << a.page_shift, (int64_t)fewest) / unit * unit);
     if (shared < a.least) shared = 0;
   }
-  if (fine)
-    for (int s = begin + (int)threadIdx.x; s < end; s += NT) a.tokens[s] = before(s) >= 0 ? shared : 0;
+  // (of a group that is none, what lies within the rows)
+  for (int s = max(begin, 0) + (int)threadIdx.x; s < min(end, a.S); s += NT) a.tokens[s] = fine && before(s) >= 0 ? shared : 0;
   if (threadIdx.x < 4) {
     const int64_t from = !fine ? 0 : a.starts ? a.starts[begin] : begin * each;
     const int64_t to = !fine ? 0 : a.starts ? a.starts[end] : end * each;

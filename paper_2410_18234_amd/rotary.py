@@ -7,7 +7,7 @@ from typing import Optional, Sequence
 
 import torch
 
-from .binding import _check, _need, _ptr, _stream, load_library
+from .binding import _check, _here, _need, _ptr, _stream, load_library
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
@@ -94,6 +94,7 @@ def rotary(x: torch.Tensor, rope: Rotary, positions: torch.Tensor, inverse: bool
         raise ValueError("x must be [T][heads][head_dim]")
     if not x.is_cuda:
         raise ValueError("x must be a GPU tensor")
+    _here(x.device)
     if x.dtype not in _DTYPES:
         raise TypeError(f"x must be float32, bfloat16 or float16, got {x.dtype}")
     T, heads, d = x.shape

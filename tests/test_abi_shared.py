@@ -67,9 +67,12 @@ def test_rotary(lib):
                          (dict(out=ODD), EINVAL), (dict(positions=none), EINVAL), (dict(r=none), EINVAL), (dict(dtype=3), EUNSUPPORTED),
                          (dict(T=-1), ESHAPE), (dict(T=(1 << 24) + 1), ESHAPE), (dict(H=0), ESHAPE), (dict(D=0), ESHAPE), (dict(D=62), ESHAPE),
                          (dict(D=65537), ESHAPE), (dict(H=1 << 25), ESHAPE), (dict(xt=-1), EINVAL), (dict(xh=-64), EINVAL), (dict(ot=63), EINVAL),
-                         (dict(oh=63), EINVAL), (dict(out=FAKE, ot=256), EINVAL), (dict(out=FAKE, xh=128), EINVAL)):
+                         (dict(oh=63), EINVAL), (dict(ot=64), EINVAL), (dict(ot=100), EINVAL), (dict(ot=64, oh=255), EINVAL), (dict(ot=127), EINVAL), (dict(out=FAKE, ot=256), EINVAL), (dict(out=FAKE, xh=128), EINVAL)):
         assert rotary(lib, **change) == code, change
     assert rotary(lib, T=0, x=none, out=none, positions=none) == 0
+    # (rows that lie apart pass these checks: the next one refuses)
+    for apart in (dict(ot=128), dict(ot=64, oh=256), dict(ot=64, T=1), dict(ot=64, H=1, D=64, oh=0)):
+        assert rotary(lib, positions=none, **apart) == EINVAL and rotary(lib, dtype=3, **apart) == EUNSUPPORTED
 
 
 def test_append(lib):
@@ -125,6 +128,24 @@ def test_python_arguments():
             setattr(rope, name, 1)
         with pytest.raises(AttributeError):
             delattr(rope, name)
+
+
+@pytest.mark.gpu
+def test_another_device_than_the_current_one(monkeypatch):
+    """(The current device's number is what the calls are told here.)"""
+    dev = torch.device("cuda:0")
+    i32 = dict(dtype=torch.int32, device=dev)
+    rope = mdss.Rotary(torch.ones(4, dtype=torch.float64, device=dev))
+    x, pos = torch.zeros((3, 2, 64), dtype=torch.bfloat16, device=dev), torch.zeros(3, **i32)
+    c = mdss.PagedCache.empty(1, 4, 2, 64, 16, device=dev)
+    table, lengths, groups = torch.zeros((3, 1), **i32), torch.ones(3, **i32), torch.tensor([0, 3], **i32)
+    shared = mdss.cache_shared(c, 3, None, table, lengths, groups)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    for call in (lambda: mdss.rotary(x, rope, pos), lambda: mdss.cache_append_rotary(c, 0, x, x, None, table, lengths, rope),
+                 lambda: mdss.cache_shared(c, 3, None, table, lengths, groups),
+                 lambda: mdss.cache_attention_shared(x, c, 0, None, table, lengths, shared)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
 
 
 @pytest.mark.gpu

@@ -189,6 +189,37 @@ def test_pages_of_unlike_scale_and_large_scores(kind):
     run(pool, c, q, q64, kind, uniform=True)
 
 
+@pytest.mark.parametrize("group", [2, 40])
+def test_queries_that_are_not_finite(group):
+    """They spoil their own row alone, whichever part of it the kernels take first."""
+    rng = np.random.default_rng([21, group])
+    c = Groups([(300, [(1, 20), (2, 70)]), (128, [(1, 1)] * 3)], 16, rng)
+    pool = oc.new_pool(1, c.pages, 1, 64, 16)
+    fill(pool, rng)
+    q, q64 = queries(rng, (c.T, group, 64), "bf16")
+    for t, hq, value in ((0, 1, math.nan), (2, 0, math.inf), (4, 1, -math.inf)):
+        q[t, hq, 5], q64[t, hq, 5] = value, value
+    out = run(pool, c, q, q64, "bf16")
+    assert sorted({tuple(x) for x in torch.nonzero(torch.isnan(out))[:, :2].tolist()}) == [(0, 1), (2, 0), (4, 1)]
+
+
+@pytest.mark.parametrize("group", [1, 8, 40])
+def test_hints_choose_no_tokens(group):
+    """Hints that are too small or far too large: the same tokens."""
+    rng = np.random.default_rng([22, group])
+    c = Groups([(1500, [(2, 300), (1, 20), (5, 40)]), (200, [(3, 700)] * 2)], 32, rng)
+    pool = oc.new_pool(1, c.pages, 1, 128, 32)
+    fill(pool, rng)
+    q, q64 = queries(rng, (c.T, group, 128), "f16")
+    cache, starts, table, lengths = to_gpu(pool), ids(c.starts), ids(c.table), ids(c.lengths)
+    shared = mdss.cache_shared(cache, c.T, starts, table, lengths, ids(c.groups))
+    want = oc.attention(pool, 0, q64, c.starts, c.table, c.lengths, 128 ** -0.5)
+    for most in ((1, 1, 1, 1), (5, 1, 64, 100000), (1, 1000, 100000, 1), (1000000, 64, 1, 64), (1, 64, 640, 0)):
+        out, lse = mdss.cache_attention_shared(q, cache, 0, starts, table, lengths, shared, want_lse=True,
+                                               **dict(zip(("max_new", "max_group", "max_shared", "max_own"), most)))
+        check(out, lse, want, "f16", 128, max(c.lengths))
+
+
 def test_strides_scales_and_a_workspace():
     rng = np.random.default_rng(18)
     c = Groups([(200, [(2, 9), (1, 30)]), (90, [(1, 2)] * 3)], 16, rng)

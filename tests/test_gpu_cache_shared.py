@@ -90,6 +90,8 @@ def test_groups_that_are_none():
         torch.cuda.synchronize()
         if not 0 <= groups[0] <= groups[1] <= 4:
             assert rows.tolist() == [[0, 0, -1, 0]]
+    tokens, rows = mdss.cache_shared(cache, c.T, ids(c.starts), ids(c.table), ids(c.lengths), ids([0, 9, 4]))
+    assert tokens.tolist() == [0] * 4 and rows.tolist() == [[0, 0, -1, 0]] * 2
     tokens, rows = mdss.cache_shared(cache, 0, ids([0]), ids(np.zeros((0, 3))), ids([]), ids([0, 0]))
     assert tokens.numel() == 0 and rows.tolist() == [[0, 0, -1, 0]]
 
