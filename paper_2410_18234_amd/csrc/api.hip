@@ -595,7 +595,7 @@ mdss_status mdss_cache_attention_shared(const mdss_cache* cache, int32_t layer, 
   const mdss::CacheView c = cache_view(cache);
   const size_t need = mdss::workspace_bytes_attention_shared(c, T, S, G, width, heads_q, !starts, max_new, max_group, max_shared,
                                                              max_own);
-  if (!workspace_ok(workspace, workspace_bytes, need)) return MDSS_EWORKSPACE;
+  if (need > 0 && !workspace_ok(workspace, workspace_bytes, need)) return MDSS_EWORKSPACE;
   const mdss::CacheRows rows = {starts, table, lengths, T, width, (int)S};
   return from_hip(mdss::launch_cache_attention_shared(c, layer, q, dtype, heads_q, q_token_stride, q_head_stride, rows, tokens,
                                                       group_rows, G, scale, max_new, max_group, max_shared, max_own, out, lse,

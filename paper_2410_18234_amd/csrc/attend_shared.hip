@@ -485,6 +485,18 @@ SharedPlan shared_plan(const CacheView& c, int64_t T, int64_t S, int64_t G, int6
   return p;
 }
 
+// Whether the rows had better go over their tokens one sequence at a time, in one launch without a join: where the caller knows that what is
+// shared is short, or the rows that share it are few.  8 cache heads of 128 and 32 query heads, apart and together: 4 rows over 1000 tokens
+// 13.7 and 19.5 us, 4 over 16000 22 and 32, 4 x 8 over 1000 14.7 and 18.7, over 4000 28.9 and 27.2, 16 x 4 over 4000 53 and 38, 64 x 4 over
+// 1000 64 and 49.  A prefix of more than 64 rows is a launch of its own: 8 x 4 rows of 5 new tokens over 2000 36 and 47, 64 rows of one over
+// 1000 62 and 69, 32 x 8 of 5 over 2000 116 and 111.
+bool apart(const CacheView& c, int64_t T, int64_t S, int64_t width, int group, int64_t max_group, int64_t max_shared) {
+  if (max_shared <= 0) return false;
+  const int64_t tiles = (at_most(max_shared, width << c.page_shift) + 63) >> 6;
+  return S * c.heads * tiles < (at_most(max_group, T) * group > 64 ? 49152 : 12288);
+}
+int64_t longest(int64_t max_shared, int64_t max_own) { return max_shared > 0 && max_own > 0 ? max_shared + max_own : 0; }
+
 template <typename Kernel>
 hipError_t shared_blocks(Kernel kernel, AttendArgs a, int64_t from, int64_t to, hipStream_t st) {
   constexpr int64_t most = (1 << 24) - 1;  // (a dimension of a launch holds less than 2^32 threads)
@@ -548,6 +560,8 @@ hipError_t launch_cache_shared(const CacheView& c, const CacheRows& rows, const 
 
 size_t workspace_bytes_attention_shared(const CacheView& c, int64_t T, int64_t S, int64_t G, int64_t width, int64_t heads_q,
                                         bool uniform, int64_t max_new, int64_t max_group, int64_t max_shared, int64_t max_own) {
+  if (apart(c, T, S, width, (int)(heads_q / c.heads), max_group, max_shared))
+    return workspace_bytes_attention(c, T, S, width, heads_q, max_new, longest(max_shared, max_own), uniform);
   const SharedPlan p = shared_plan(c, T, S, G, width, (int)(heads_q / c.heads), uniform, max_new, max_group, max_shared, max_own);
   return (size_t)T * heads_q * (p.pre_splits + p.splits) * (c.d + 2) * sizeof(float);
 }
@@ -556,6 +570,9 @@ hipError_t launch_cache_attention_shared(const CacheView& c, int layer, const vo
                                          int64_t q_sh, const CacheRows& rows, const int32_t* tokens, const int32_t* groups, int64_t G,
                                          float scale, int64_t max_new, int64_t max_group, int64_t max_shared, int64_t max_own,
                                          void* out, float* lse, void* workspace, hipStream_t st) {
+  if (apart(c, rows.T, rows.S, rows.width, (int)(heads_q / c.heads), max_group, max_shared))
+    return launch_cache_attention(c, layer, q, dtype, heads_q, q_st, q_sh, rows, scale, max_new, longest(max_shared, max_own), out, lse,
+                                  workspace, st);
   const SharedPlan p = shared_plan(c, rows.T, rows.S, G, rows.width, (int)(heads_q / c.heads), rows.starts == nullptr, max_new,
                                    max_group, max_shared, max_own);
   AttendArgs a = attend_args(c, layer, q, heads_q, q_st, q_sh, rows, scale, out, lse, workspace, p.pre_splits + p.splits);

@@ -203,6 +203,36 @@ def test_queries_that_are_not_finite(group):
     assert sorted({tuple(x) for x in torch.nonzero(torch.isnan(out))[:, :2].tolist()}) == [(0, 1), (2, 0), (4, 1)]
 
 
+@pytest.mark.parametrize("G,W,n,heads,group,d,prefix", [(5, 8, 1, 8, 2, 64, 3000), (5, 8, 1, 8, 8, 128, 3000), (4, 6, 2, 8, 1, 96, 5000), (2, 3, 1, 8, 4, 256, 20000),
+                                                        (2, 40, 1, 8, 2, 64, 5100), (2, 40, 1, 8, 4, 128, 5100), (1, 10, 4, 8, 1, 128, 12000)])
+def test_calls_that_are_large_enough_to_go_together(G, W, n, heads, group, d, prefix):
+    """With every hint, so that prefixes and own tokens are cut as a program's are, by each kernel."""
+    rng = np.random.default_rng([G, W, n, group, d])
+    c = Groups([(prefix - 700 * g, [(n, n + int(x)) for x in rng.integers(0, 90, W)]) for g in range(G)], 64, rng)
+    pool = oc.new_pool(1, c.pages, heads, d, 64)
+    fill(pool, rng)
+    q, q64 = queries(rng, (c.T, heads * group, d), "bf16")
+    cache, starts, table, lengths = to_gpu(pool), ids(c.starts), ids(c.table), ids(c.lengths)
+    shared = mdss.cache_shared(cache, c.T, starts, table, lengths, ids(c.groups))
+    most = hints(c, shared[0].tolist(), shared[1].tolist())
+    assert len(c.new) * heads * (most["max_shared"] // 64) >= (49152 if most["max_group"] * group > 64 else 12288)
+    out, lse = mdss.cache_attention_shared(q, cache, 0, starts, table, lengths, shared, want_lse=True, **most)
+    torch.cuda.synchronize()
+    rows = rng.choice(len(c.new), 4, replace=False)  # (the oracle takes its time: some of the sequences)
+    for s in rows:
+        own = slice(c.starts[s], c.starts[s + 1])
+        want = oc.attention(pool, 0, q64[own], [0, n], c.table[s:s + 1], c.lengths[s:s + 1], d ** -0.5)
+        check(out[own], lse[own], want, "bf16", d, max(c.lengths))
+    # The others against the call that knows no prefixes: both are within the bound of the same values, whose sums of p |v| are
+    # attention over the values without their signs (2^-8 off at most itself).  Scores are off by 2 (d 2^-24 15 + 63 2^-24) < 2^-11
+    # here, since |scale| |q| . |k| is below 15 (256 elements of 1 and 4 at most in q, of some 1 in k, times 1/16).
+    plain, plse = mdss.cache_attention(q, cache, 0, starts, table, lengths, want_lse=True)
+    mag = mdss.cache_attention(q, mdss.PagedCache(cache.k, cache.v & 127, cache.k_exp, cache.v_exp), 0, starts, table, lengths).float()
+    bound = 1.02 * mag * (2.0 ** -10 + (max(c.lengths) + 64) * 2.0 ** -24) + 1.01 * 2.0 ** -8 * plain.float().abs()
+    assert bool(((out.float() - plain.float()).abs() <= 2 * bound).all())
+    assert bool(((lse - plse).abs() <= 2 * (2.0 ** -11 + (max(c.lengths) + 64) * 2.0 ** -24 + 2.0 ** -22 * (plse.abs() + 30.0))).all())
+
+
 @pytest.mark.parametrize("group", [1, 8, 40])
 def test_hints_choose_no_tokens(group):
     """Hints that are too small or far too large: the same tokens."""
