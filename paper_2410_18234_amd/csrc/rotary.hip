@@ -21,7 +21,8 @@ struct RotaryArgs {
 
 // A thread has one unit of a token and goes over some of its heads, so an angle is formed once for them; four heads at a time are
 // in flight.  WIDE: a unit is 16 bytes of both halves (or of a row of side by side pairs), else one pair or one element.
-// Bound by memory.
+// Bound by memory on prompts (8192 tokens of 40 heads of 128, f16, 168 MB: 30.4 to 32.5 us, 5.2 to 5.5 TB/s; the angles keep vector
+// instructions at 32 % of the cycles), by the launch on a step (64 tokens of 40 heads: 3.8 us, a call 9.2 us).
 template <int KIND, bool WIDE, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
   using P = Pack<KIND>;
