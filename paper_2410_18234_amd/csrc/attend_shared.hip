@@ -483,8 +483,9 @@ SharedPlan shared_plan(const CacheView& c, int64_t T, int64_t S, int64_t G, int6
   if (pre_splits > pre_tiles / least) pre_splits = pre_tiles / least;
   cut(pre_tiles, pre_splits, &p.pre_splits, &p.pre_split_tiles);
   // Own tokens: a wave for each (sequence, head) where there are enough of them (128 sequences of up to 150 tokens, 8 heads: 21.7 us, 24.1 with
-  // four waves each; of 600: 44 and 47.5; 32 sequences of 600: 22.5 and 20.4), else four waves, split as long as CUs are left.
-  p.own_waves = !p.wide && own >= 1024 ? 1 : 4;
+  // four waves each; of 600: 44 and 47.5; 32 sequences of 600: 22.5 and 20.4) or where they are too few tiles for four (96 sequences of up to 45 tokens
+  // behind prefixes: 62 us, 64 with four), else four waves, split as long as CUs are left.
+  p.own_waves = !p.wide && (own >= 1024 || tiles <= 2) ? 1 : 4;
   int64_t splits = p.own_waves == 1 ? 1 : 512 / own;
   if (splits > tiles / 8) splits = tiles / 8;
   cut(tiles, splits, &p.splits, &p.split_tiles);
