@@ -662,7 +662,7 @@ mdss_status mdss_rotary(const void* x, int64_t x_token_stride, int64_t x_head_st
  * with a NaN or infinity becomes two NaN codes, of either sign.
  * q [T][heads_q][head_dim] (heads_q 0: none; a multiple of heads, at most 1024 per
  * head, T * heads_q < 2^31): queries of dtype, which go to q_out (contiguous,
- * 16-byte aligned, apart from q) turned by the same positions, also for rows
+ * 16-byte aligned, apart from q, key and value) turned by the same positions, also for rows
  * without a page; tokens of no sequence are not written. */
 mdss_status mdss_cache_append_rotary(const mdss_cache* cache, int32_t layer, const void* key, int64_t key_token_stride,
                                      int64_t key_head_stride, const void* value, int64_t value_token_stride,

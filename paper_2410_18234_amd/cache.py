@@ -234,7 +234,8 @@ def cache_attention_shared(q: torch.Tensor, cache: PagedCache, layer: int, start
                            max_shared: int = 0, max_own: int = 0, want_lse: bool = False, out: Optional[torch.Tensor] = None,
                            workspace: Optional[torch.Tensor] = None):
     """``cache_attention`` that reads what a group of rows shares once for all of them; ``shared`` is what ``cache_shared`` returned
-    for these starts and tables (one result serves every layer, and later steps while tables keep their leading pages).
+    for these starts and tables (one result serves every layer, and later steps with as many new tokens, while tables keep their
+    leading pages and no length falls).
 
     ``max_new`` (of a sequence), ``max_group`` (new tokens of a group), ``max_shared`` and ``max_own`` (a sequence's tokens past the
     shared ones) say how many there are at most (0: unknown); they only choose how the work is cut."""
