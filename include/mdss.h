@@ -682,7 +682,9 @@ mdss_status mdss_cache_append_rotary(const mdss_cache* cache, int32_t layer, con
  *   tokens [S]: what row s shares (0: takes no part, or is in no group)
  *   group_rows [G][4]: the group's first new token and their count (starts of its
  *   rows; T / S each where starts is NULL), the first row that takes part (-1: none), the
- *   shared tokens.  (A group whose rows are not within [0, S]: 0, 0, -1, 0.)
+ *   shared tokens.
+ * Bounds that do not ascend within [0, S], or begin before an earlier group's end (lists padded with zeros), are no group:
+ * its row is the first token behind the groups before it, 0, -1, 0, and no row takes part by it.
  * G in [0, MDSS_MAX_B], least >= 0. */
 mdss_status mdss_cache_shared(const mdss_cache* cache, int64_t T, const int32_t* starts, const int32_t* table, int64_t width,
                               const int32_t* lengths, int64_t S, const int32_t* groups, int64_t G, int32_t least,

@@ -163,10 +163,17 @@ def attention(pool, layer, q, starts, table, lengths, scale):
 
 
 def shared(pages, ps, starts, table, lengths, groups, least=0):
-    """(tokens [S], group rows [G][4]) of rows groups[g] .. groups[g + 1] - 1; starts [S + 1]."""
+    """(tokens [S], group rows [G][4]) of rows groups[g] .. groups[g + 1] - 1; starts [S + 1].  Bounds that do not ascend within the
+    rows are no group, nor is one that begins before an earlier one's end: none of its rows, first token where those before end."""
     S, width = table.shape
-    tokens, rows = [0] * S, []
+    tokens, rows, reach = [0] * S, [], 0
     for a, b in zip(groups[:-1], groups[1:]):
+        ordered = 0 <= a <= b <= S
+        if not ordered or a < reach:
+            rows.append([int(starts[reach]), 0, -1, 0])
+            reach = max(reach, b) if ordered else reach
+            continue
+        reach = b
         held = {s: min(int(lengths[s]), width * ps) - int(starts[s + 1] - starts[s]) for s in range(a, b)}
         part = [s for s in range(a, b) if held[s] >= max(1, least)]
         n = 0

@@ -212,7 +212,9 @@ def cache_shared(cache: PagedCache, T: int, starts: Optional[torch.Tensor], tabl
 
     ``T`` new tokens in all.  Rows take part that hold ``least`` tokens (at least one) before their new ones; their shared tokens are the
     leading pages that are the same in all of them, in whole multiples of ``max(64, page_size)``, 0 where that is less than
-    ``least``.  A group's row: its first new token, its new tokens, its first row that takes part (-1: none), its shared tokens."""
+    ``least``.  A group's row: its first new token, its new tokens, its first row that takes part (-1: none), its shared tokens.
+    Bounds that do not ascend within the rows, or begin before an earlier group's end (padding by zeros), are no group: no row takes
+    part by it."""
     lib = load_library()
     _here(cache.device)
     S, width = _rows(cache, starts, table, lengths)

@@ -15,30 +15,34 @@ struct SharedArgs {
   int32_t *tokens, *rows;
   int64_t T, width, pages;
   int S, G, page_shift, least;
+  int each;  // groups of a workgroup
 };
 
-// A workgroup a group.  It finds who takes part (the first one, the fewest tokens before the new ones), then compares the others' pages
-// with the first one's, a wave a row at a time, up to the first difference that any wave has met.  Bound by the chain groups -
-// lengths - table (4 rows: 4.4 us; 128 groups of 8 rows: 7.4 us, calls of 12.7 and 13.0 us).
+// A workgroup a group (beyond 4096 of them, several in turn).  It finds who takes part (the first one, the fewest tokens before the new ones),
+// then compares the others' pages with the first one's, a wave a row at a time, up to the first difference that any wave has met.  Bound by
+// the chain groups - lengths - table (4 rows: 4.6 us; 128 groups of 8 rows: 7.6 us).
+//
+// Bounds are the caller's, and may not ascend.  What ascends is `reach`, the largest end of the groups before (a group: bounds that ascend
+// within the rows); one that begins before it would take rows of an earlier one, and is none.  Group g writes the tokens of the rows
+// reach(g) .. reach(g + 1) - 1, so each row has one writer, and its first token is that of a row from reach(g) on, so these ascend
+// whatever the bounds: attention's search for the group of a row tile counts on it.
 template <int NT>
 __global__ __launch_bounds__(NT) void shared_kernel(const SharedArgs a) {
-  __shared__ int first_row, fewest, count, common;
+  __shared__ int first_row, fewest, count, common, reach_before;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int g = blockIdx.x;
-  if (g == 0) {  // rows of no group
-    const int end = a.G > 0 ? min(max(a.groups[0], 0), a.S) : a.S;
-    for (int s = threadIdx.x; s < end; s += NT) a.tokens[s] = 0;
-  }
-  if (a.G == 0) return;
-  if (g == a.G - 1)
-    for (int s = min(max(a.groups[a.G], 0), a.S) + threadIdx.x; s < a.S; s += NT) a.tokens[s] = 0;
-  const int begin = a.groups[g], end = a.groups[g + 1];
-  const bool fine = begin >= 0 && begin <= end && end <= a.S;
+  const int g0 = blockIdx.x * a.each, g1 = min(a.G, g0 + a.each);
+  const auto is_group = [&](int begin, int end) { return begin >= 0 && begin <= end && end <= a.S; };
   if (threadIdx.x == 0) {
     first_row = fewest = INT32_MAX;
-    count = 0;
+    count = reach_before = 0;
   }
   __syncthreads();
+  // (a bound of the groups before this one for each thread: on its way until it is asked for at the end)
+  int bound0 = 0, bound1 = 0;
+  if (a.G > 0) {
+    bound0 = a.groups[min((int)threadIdx.x, g0)];
+    bound1 = a.groups[min((int)threadIdx.x, g0) + 1];
+  }
   const int64_t most = a.width << a.page_shift, each = a.S > 0 ? a.T / a.S : 0;
   // tokens before the new ones; -1 for who takes no part
   const auto before = [&](int s) {
@@ -46,66 +50,97 @@ __global__ __launch_bounds__(NT) void shared_kernel(const SharedArgs a) {
     const int64_t b = min((int64_t)a.lengths[s], most) - n;
     return b >= max(a.least, 1) ? (int)min(b, (int64_t)INT32_MAX) : -1;
   };
-  if (fine) {
-    int r = INT32_MAX, few = INT32_MAX, some = 0;
-    for (int s = begin + (int)threadIdx.x; s < end; s += NT) {
-      const int b = before(s);
-      if (b < 0) continue;
-      r = min(r, s);
-      few = min(few, b);
-      ++some;
+  int reach = 0;
+  for (int g = g0; g < g1; ++g) {
+    const int begin = a.groups[g], end = a.groups[g + 1];
+    if (g > g0) {
+      __syncthreads();  // (the last group's words are read)
+      if (threadIdx.x == 0) {
+        first_row = fewest = INT32_MAX;
+        count = 0;
+      }
+      __syncthreads();
     }
-    if (some > 0) {
-      atomicMin(&first_row, r);
-      atomicMin(&fewest, few);
-      atomicAdd(&count, some);
+    const bool ordered = is_group(begin, end);
+    if (ordered) {
+      int r = INT32_MAX, few = INT32_MAX, n = 0;
+      for (int s = begin + (int)threadIdx.x; s < end; s += NT) {
+        const int b = before(s);
+        if (b < 0) continue;
+        r = min(r, s);
+        few = min(few, b);
+        ++n;
+      }
+      if (n > 0) {
+        atomicMin(&first_row, r);
+        atomicMin(&fewest, few);
+        atomicAdd(&count, n);
+      }
     }
-  }
-  __syncthreads();
-  const int lead = first_row;
-  if (threadIdx.x == 0) common = count > 1 ? (fewest + (1 << a.page_shift) - 1) >> a.page_shift : 0;
-  __syncthreads();
-  if (count > 1) {
-    const int32_t* mine = a.table + (int64_t)lead * a.width;
-    for (int s = begin + wave; s < end; s += NT / 64) {
-      if (before(s) < 0) continue;
-      const int32_t* row = a.table + (int64_t)s * a.width;
-      // (the shared bound only sinks: a wave that reads an old one compares more than it has to)
-      for (int j0 = 0; j0 < *(volatile int*)&common; j0 += 256) {
-        bool differ[4];
+    __syncthreads();
+    const int lead = first_row;
+    const bool some = count > 1;
+    if (threadIdx.x == 0) common = some ? (fewest + (1 << a.page_shift) - 1) >> a.page_shift : 0;
+    __syncthreads();
+    if (some) {
+      const int32_t* mine = a.table + (int64_t)lead * a.width;
+      for (int s = begin + wave; s < end; s += NT / 64) {
+        if (before(s) < 0) continue;
+        const int32_t* row = a.table + (int64_t)s * a.width;
+        // (the shared bound only sinks: a wave that reads an old one compares more than it has to)
+        for (int j0 = 0; j0 < *(volatile int*)&common; j0 += 256) {
+          bool differ[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int64_t j = min((int64_t)(j0 + 64 * i + lane), a.width - 1);
-          differ[i] = row[j] != mine[j] || (uint32_t)mine[j] >= (uint64_t)a.pages;
-        }
-        int at = -1;
+          for (int i = 0; i < 4; ++i) {
+            const int64_t j = min((int64_t)(j0 + 64 * i + lane), a.width - 1);
+            differ[i] = row[j] != mine[j] || (uint32_t)mine[j] >= (uint64_t)a.pages;
+          }
+          int at = -1;
 #pragma unroll
-        for (int i = 3; i >= 0; --i) {
-          const uint64_t hit = __ballot(differ[i]);
-          if (hit) at = j0 + 64 * i + __ffsll((unsigned long long)hit) - 1;
-        }
-        if (at >= 0) {
-          if (lane == 0) atomicMin(&common, at);
-          break;
+          for (int i = 3; i >= 0; --i) {
+            const uint64_t hit = __ballot(differ[i]);
+            if (hit) at = j0 + 64 * i + __ffsll((unsigned long long)hit) - 1;
+          }
+          if (at >= 0) {
+            if (lane == 0) atomicMin(&common, at);
+            break;
+          }
         }
       }
     }
+    if (g == g0 && g0 > 0) {
+      int most_before = (int)threadIdx.x < g0 && is_group(bound0, bound1) ? bound1 : 0;
+#pragma unroll 4
+      for (int i = threadIdx.x + NT; i < g0; i += NT) {
+        bound0 = a.groups[i];
+        bound1 = a.groups[i + 1];
+        most_before = is_group(bound0, bound1) ? max(most_before, bound1) : most_before;
+      }
+      most_before = (int)wave_max((float)most_before);  // (rows are fewer than 2^24)
+      if (lane == 0) atomicMax(&reach_before, most_before);
+    }
+    __syncthreads();
+    if (g == g0) reach = reach_before;
+    const bool fine = ordered && begin >= reach;
+    const int unit = max(64, 1 << a.page_shift);
+    int shared = 0;
+    if (fine && some) {
+      shared = (int)(min((int64_t)common << a.page_shift, (int64_t)fewest) / unit * unit);
+      if (shared < a.least) shared = 0;
+    }
+    const int next = ordered ? max(reach, end) : reach;
+    for (int s = reach + (int)threadIdx.x; s < next; s += NT) a.tokens[s] = fine && s >= begin && before(s) >= 0 ? shared : 0;
+    if (threadIdx.x < 4) {
+      const int at = fine ? begin : reach, upto = fine ? end : reach;
+      const int64_t from = a.starts ? a.starts[at] : at * each;
+      const int64_t to = a.starts ? a.starts[upto] : upto * each;
+      const int word = threadIdx.x;
+      a.rows[4 * (int64_t)g + word] = word == 0 ? (int)from : word == 1 ? (int)(to - from) : word == 2 ? (fine && lead < INT32_MAX ? lead : -1) : shared;
+    }
+    reach = next;
   }
-  __syncthreads();
-  const int unit = max(64, 1 << a.page_shift);
-  int shared = 0;
-  if (count > 1) {
-    shared = (int)(min((int64_t)common << a.page_shift, (int64_t)fewest) / unit * unit);
-    if (shared < a.least) shared = 0;
-  }
-  // (of a group that is none, what lies within the rows)
-  for (int s = max(begin, 0) + (int)threadIdx.x; s < min(end, a.S); s += NT) a.tokens[s] = fine && before(s) >= 0 ? shared : 0;
-  if (threadIdx.x < 4) {
-    const int64_t from = !fine ? 0 : a.starts ? a.starts[begin] : begin * each;
-    const int64_t to = !fine ? 0 : a.starts ? a.starts[end] : end * each;
-    const int word = threadIdx.x;
-    a.rows[4 * (int64_t)g + word] = word == 0 ? (int)from : word == 1 ? (int)(to - from) : word == 2 ? (lead < INT32_MAX ? lead : -1) : shared;
-  }
+  if (g1 == a.G)  // rows past the last group
+    for (int s = reach + (int)threadIdx.x; s < a.S; s += NT) a.tokens[s] = 0;
 }
 
 // ---------------------------------------------------------------- attention
@@ -555,9 +590,11 @@ hipError_t shared_launch(const AttendArgs& a, const SharedPlan& p, hipStream_t s
 
 hipError_t launch_cache_shared(const CacheView& c, const CacheRows& rows, const int32_t* groups, int64_t G, int32_t least,
                                int32_t* tokens, int32_t* group_rows, hipStream_t st) {
-  const SharedArgs a = {rows.starts, rows.table, rows.lengths, groups,  tokens, group_rows, rows.T,
-                        rows.width,  c.pages,    rows.S,       (int)G, c.page_shift, least};
-  const unsigned grid = G > 0 ? (unsigned)G : 1u;
+  // (each workgroup reads the bounds before its own: as many workgroups as groups would read G^2 / 2 of them)
+  const int64_t each = (G + 4095) / 4096;
+  const SharedArgs a = {rows.starts, rows.table, rows.lengths, groups,       tokens, group_rows, rows.T,
+                        rows.width,  c.pages,    rows.S,       (int)G,       c.page_shift, least, (int)(each > 0 ? each : 1)};
+  const unsigned grid = G > 0 ? (unsigned)((G + each - 1) / each) : 1u;
   if (rows.S > 16 * (G > 0 ? G : 1))
     shared_kernel<1024><<<grid, 1024, 0, st>>>(a);
   else
