@@ -698,8 +698,9 @@ mdss_status mdss_cache_shared(const mdss_cache* cache, int64_t T, const int32_t*
  * keep their leading pages and no length falls.  tokens[s] = 0: the row reads all of its own.
  * max_new (of a sequence), max_group (new tokens of a group), max_shared and
  * max_own (a sequence's tokens past the shared ones) are host-side hints on the
- * most there are (0: none); they choose how the work is cut, and whether sequences go over what they
- * share together at all (where it is short, or few share it, they do not).
+ * most there are (0: unknown); they choose how the work is cut, and whether sequences go over what they
+ * share together at all: where it is short, or few share it, they do not, and the call is mdss_cache_attention's.
+ * max_shared from 1 to 63 says that nothing is shared.
  * workspace: at least mdss_workspace_bytes_attention_shared(...) bytes, 256-byte aligned (may be NULL if that is 0): head_dim + 2
  * floats for each part of a row of T * heads_q, which are two and more (a call for new tokens by the few, not for long prompts). */
 size_t mdss_workspace_bytes_attention_shared(const mdss_cache* cache, int64_t T, int64_t S, int64_t G, int64_t width, int64_t heads_q,

@@ -240,7 +240,9 @@ def cache_attention_shared(q: torch.Tensor, cache: PagedCache, layer: int, start
     leading pages and no length falls).
 
     ``max_new`` (of a sequence), ``max_group`` (new tokens of a group), ``max_shared`` and ``max_own`` (a sequence's tokens past the
-    shared ones) say how many there are at most (0: unknown); they only choose how the work is cut."""
+    shared ones) say how many there are at most (0: unknown); they choose how the work is cut, and whether what is shared is read
+    together at all: where it is short, or few share it, the call goes as ``cache_attention``'s.  ``max_shared`` from 1 to 63 says that
+    nothing is shared."""
     lib = load_library()
     _here(cache.device)
     S, width = _rows(cache, starts, table, lengths)

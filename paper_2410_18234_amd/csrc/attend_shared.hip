@@ -534,6 +534,7 @@ SharedPlan shared_plan(const CacheView& c, int64_t T, int64_t S, int64_t G, int6
 // 1000 62 and 69, 32 x 8 of 5 over 2000 116 and 111.
 bool apart(const CacheView& c, int64_t T, int64_t S, int64_t width, int group, int64_t max_group, int64_t max_shared) {
   if (max_shared <= 0) return false;
+  if (max_shared < 64) return true;  // (what is shared comes in whole tiles: nothing is)
   const int64_t tiles = (at_most(max_shared, width << c.page_shift) + 63) >> 6;
   return S * c.heads * tiles < (at_most(max_group, T) * group > 64 ? 49152 : 12288);
 }
