@@ -287,12 +287,15 @@ __global__ __launch_bounds__(NT, 4) void append_kernel(const AppendArgs a) {
   const int key_total = TURN ? total / 2 : total;
   const auto fetch_v = [&](int e) { return load8(vx + (int64_t)(e / kLine) * a.val_st + (e % kLine) * 8, a.val_al); };
 
-  // the largest magnitudes
+  // the largest magnitudes (without TURN keys and values go under one condition: 44 us on the prompts above, 45.5 under two)
   u32x4 kh[kHeld], vh[kHeld];
 #pragma unroll
   for (int j = 0; j < kHeld; ++j) {
-    if (key_place(j) < key_total) kh[j] = fetch_k(key_piece(j, key_place(j)));
-    if (tid + NT * j < total) vh[j] = fetch_v(tid + NT * j);
+    if (TURN && key_place(j) < key_total) kh[j] = fetch_k(key_piece(j, key_place(j)));
+    if (tid + NT * j < total) {
+      if (!TURN) kh[j] = fetch_k(tid + NT * j);
+      vh[j] = fetch_v(tid + NT * j);
+    }
   }
   int ke = kCacheMinExp, ve = kCacheMinExp;  // of the page's earlier tokens
   if (o > 0) {
@@ -321,8 +324,11 @@ __global__ __launch_bounds__(NT, 4) void append_kernel(const AppendArgs a) {
   float km = 0.0f, vm = 0.0f;
 #pragma unroll
   for (int j = 0; j < kHeld; ++j) {
-    if (key_place(j) < key_total) km = largest_key(kh[j], key_piece(j, key_place(j)), km);
-    if (tid + NT * j < total) vm = largest(vh[j], vm);
+    if (TURN && key_place(j) < key_total) km = largest_key(kh[j], key_piece(j, key_place(j)), km);
+    if (tid + NT * j < total) {
+      if (!TURN) km = largest(kh[j], km);
+      vm = largest(vh[j], vm);
+    }
   }
   for (int e = tid + NT * kHeld; e < total; e += NT) {
     if (!TURN) km = largest(fetch_k(e), km);
