@@ -13,7 +13,10 @@
 //   p = 2^(t - M + kLift) <= 2^15 carries the value's scale,
 //   l = sum p 2^-ve the softmax's sum in the same frame (fp32), out = sum p code / l.
 // (c_g = scale log2(e) 2^ke is the lane's, so t is one fused multiply-add.)
-// The matrix cores take p in f16, which holds 11 bits of it down to 2^-14: 2^-29 of the largest.  Smaller ones matter where the
+// The matrix cores take p in f16, which holds 11 bits of it down to 2^-14: 2^-29 of the largest.  11 bits are as many as the finer
+// output type has: with a second product of what f16 leaves, p - f16(p), the error against 64 bits goes from 2.17e-4 to 2.08e-4 of the
+// result in f16 (its own rounding) and stays 1.66e-3 in bf16, and time from 46.5 to 50 us (16 groups of 8 rows over up to 6000 shared tokens,
+// 8 heads of 128), 57 to 62 (32 x 4 drafts of up to 5 tokens over up to 4000), 92 to 118 (2048 rows a head over 8192).  Smaller ones matter where the
 // tokens that lead hold values near zero, or a page has a much larger scale: where what f16 drops could reach 2^-16 of a row's
 // largest element (`lacks`) a wave goes over its tokens again (PRECISE), and it goes through a product of its own in a frame of its
 // own (left_of_low).  That costs such a wave more than its first pass; doing it in the one pass, in every tile that has smaller
@@ -53,7 +56,7 @@ struct AttendArgs {
   bool negative;
   // calls with shared prefixes: workgroups of the prefixes first, then (from pre_blocks on) those of the sequences' own tokens
   const int32_t *tokens, *groups;  // tokens [S]: those a sequence reads with its group; groups [G][4]: first new token, new tokens, row, tokens
-  int64_t block0, pre_blocks;      // (blocks: of workgroups, or where own_waves is 1, of waves past pre_blocks)
+  int64_t block0, pre_blocks;      // the launch's first workgroup, and how many take prefixes (where own_waves is 1 the others take four slots each)
   int G, pre_slots, slots, pre_splits, pre_split_tiles, own_waves;
 };
 

@@ -145,9 +145,9 @@ __global__ __launch_bounds__(NT) void shared_kernel(const SharedArgs a) {
 
 // ---------------------------------------------------------------- attention
 // Few rows: four waves that take the same rows against tiles in turn (a prefix; own tokens of few sequences), or a wave for each
-// (sequence, head), which has no partners to wait for and to join: 2048 sequences of one token of their own past the prefix.  Bound by memory
-// and the unlike lengths of what the workgroups get (heads of 128, 8 of them, four query heads each: 16 groups of 8 rows, up to 6000 shared tokens, 46 to 48 us,
-// two thirds of the copy's rate, vector instructions 38 % of the cycles, matrix instructions 12 %; 256 sequences' own tokens behind 8192 shared ones
+// (sequence, head), which has no partners to wait for and to join: 2048 sequences of one token of their own past the prefix.  Bound by memory,
+// at two thirds of the copy's rate (heads of 128, 8 of them, four query heads each: 16 groups of 8 rows, up to 6000 shared tokens, 46 to 48 us,
+// vector instructions 38 % of the cycles, matrix instructions 12 %; 256 sequences' own tokens behind 8192 shared ones
 // 70 us, 4.1 TB/s).
 template <int D, bool BF, int MT, int NW>
 __device__ __forceinline__ void shared_rows(const AttendArgs& a, const Place& p, float* joined, float* joined_ml,
