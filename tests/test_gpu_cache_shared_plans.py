@@ -51,7 +51,7 @@ def widened(c, columns):
 
 @pytest.mark.parametrize("d,group", [(64, 1), (128, 8), (128, 40), (256, 3)])
 @pytest.mark.parametrize("most", [(1, 1, 0, 1), (5, 1, 0, 100000), (1, 1000, 0, 1), (1000000, 64, 0, 64), (0, 1, 9000, 1), (1, 1, 100000, 0), (0, 0, 100000, 64),
-                                  (2, 5, 26000, 30)])
+                                  (2, 1, 26000, 30)])
 def test_hints_choose_no_tokens(most, d, group):
     """Hints that are too small or far too large, in calls that go over what they share together."""
     most = dict(zip(("max_new", "max_group", "max_shared", "max_own"), most))
@@ -59,8 +59,6 @@ def test_hints_choose_no_tokens(most, d, group):
     # (96 sequences of a head: 9000 tokens are 13536 of their tiles, the table's 32768 are 49152)
     c = Groups([(9500, [(2, 300), (1, 20), (5, 40)]), (200, [(3, 700)] * 2)] + [(64, [(1, 1 + i) for i in range(13)]) for _ in range(7)], 32, rng)
     widened(c, 1024)
-    if not together(c, 1, group, **most):
-        pytest.skip("apart")
     pool = oc.new_pool(1, c.pages, 1, d, 32)
     fill(pool, rng)
     q, q64 = queries(rng, (c.T, group, d), "f16")
